@@ -9,7 +9,8 @@
  *
  * and the variants of these steps that scaling recipes build on (transposed operands,
  * per-channel factors, single-pass cast with a factor from past maxima, strict and
- * stochastic conversion, dequantize).
+ * stochastic conversion, dequantize), and the feed-forward operators around its products (bias, activation
+ * and residual in the epilogue, the gated block, both with their backward passes; gradient norm and clipping).
  *
  * General rules for every entry point
  *   - Pointers are DEVICE pointers unless the name ends in _host.  The caller owns
@@ -393,6 +394,97 @@ int fp8_scaled_gemm(const void* a, const void* b, int in_dtype, int transA, int 
                     int64_t M, int64_t N, int64_t K, int fmtA, int fmtB,
                     uint8_t* qa_out, uint8_t* qb_out, float* amax_out, float* scale_out, void* workspace,
                     void* C, int out_dtype, int flags, void* stream);
+
+/*
+ * ---- Products with an operator behind them: the feed-forward part of a transformer ----------------
+ *
+ * The activations.  SILU: z / (1 + e^-z); GELU: z Phi(z) with the normal distribution's Phi; GELU_TANH: its form
+ * z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2; RELU: max(z, 0), derivative 0 at 0.  act(-inf) is 0 (NONE: -inf), act(NaN) is NaN.
+ */
+typedef enum { FP8_ACT_NONE = 0, FP8_ACT_RELU = 1, FP8_ACT_GELU = 2, FP8_ACT_GELU_TANH = 3, FP8_ACT_SILU = 4 } fp8_act_t;
+
+/*
+ * fp8_gemm_act -- a product with bias, activation and residual in its epilogue:
+ *     z_ij = (sum_k a_ik b_kj) / (sA_i * sB_j) + bias_j
+ *     y_ij = act(z_ij) + residual_ij
+ *     D_ij = cast_out(y_ij), or encode(fl32(y_ij * sD)) for FP8 kinds;  Z_ij = cast(z_ij);  amax = max |y_ij|
+ * A, B, D, M, N, K, factors, amax_out and flags: as for fp8_gemm_fused, bounds too (of z; everything behind it is computed in 32 bits
+ * and rounded once).
+ *   bias      device, N values of bias_dtype (fp8_dtype_t), or NULL
+ *   residual  device, M x N of residual_dtype, or NULL; may be D itself where the types are the same (D += ...), and must not
+ *             overlap it otherwise
+ *   Z         device, M x N of Z_dtype, or NULL: what the backward pass needs.  Z must not overlap any other argument.
+ * The type of an argument that is NULL is not looked at.  K = 0: the sums are +0.
+ */
+int fp8_gemm_act(const uint8_t* A, int fmtA, int transA, const uint8_t* B, int fmtB, int transB,
+                 void* D, int out_kind, int64_t M, int64_t N, int64_t K,
+                 const float* sA_dev, int64_t nsA, const float* sB_dev, int64_t nsB, int act,
+                 const void* bias, int bias_dtype, const void* residual, int residual_dtype, void* Z, int Z_dtype,
+                 const float* sD_dev, float* amax_out, int flags, void* stream);
+
+/*
+ * fp8_gemm_act_grad -- the backward pass of bias and activation in the epilogue of the data gradient that arrives there:
+ *     y_ij = (sum_k a_ik b_kj) / (sA_i * sB_j) * act'(Z_ij);   dbias_j = sum_i y_ij
+ *     D_ij = cast_out(y_ij), or encode(fl32(y_ij * sD)) for FP8 kinds;  amax = max |y_ij|
+ * (A: the gradient of the next layer's output, B: that layer's weight.)
+ *   Z          device, M x N of Z_dtype, as fp8_gemm_act kept it; may be D itself where the types are the same
+ *   dbias      device, N fp32 values, or NULL.  Written, not accumulated; sums of y in 32 bits, in the same order in every run.
+ *   workspace  device, 4-byte aligned, at least fp8_gemm_act_grad_workspace_size(M, N) bytes = 4 N for every 32 rows; contents on
+ *              entry are irrelevant.  Only looked at where dbias is given.
+ */
+size_t fp8_gemm_act_grad_workspace_size(int64_t M, int64_t N);
+int fp8_gemm_act_grad(const uint8_t* A, int fmtA, int transA, const uint8_t* B, int fmtB, int transB,
+                      void* D, int out_kind, int64_t M, int64_t N, int64_t K,
+                      const float* sA_dev, int64_t nsA, const float* sB_dev, int64_t nsB, int act,
+                      const void* Z, int Z_dtype, float* dbias, void* workspace, size_t workspace_bytes,
+                      const float* sD_dev, float* amax_out, int flags, void* stream);
+
+/*
+ * fp8_gemm_gated -- both projections of a gated feed-forward block, the activation and the product in one kernel:
+ *     [g | u] = (op(A) op(B)) / (sA * sB),  y_ij = act(g_ij) * u_ij
+ *     H_ij = cast_out(y_ij), or encode(fl32(y_ij * sH)) for FP8 kinds;  GU = cast([g | u]);  amax = max |y_ij|
+ *   B    both weights in one matrix, the gate's columns first: K x 2F (transB = 0), or 2F x K (transB = 1)
+ *   H    device, M x F of out_kind
+ *   sB_dev  nsB values: 1, 2 (of the gate, of the other projection) or 2F (one per column of op(B))
+ *   GU   device, M x 2F of GU_dtype, or NULL: what the backward pass needs
+ * The rest as for fp8_gemm_act.
+ */
+int fp8_gemm_gated(const uint8_t* A, int fmtA, int transA, const uint8_t* B, int fmtB, int transB,
+                   void* H, int out_kind, int64_t M, int64_t F, int64_t K,
+                   const float* sA_dev, int64_t nsA, const float* sB_dev, int64_t nsB, int act,
+                   void* GU, int GU_dtype, const float* sH_dev, float* amax_out, int flags, void* stream);
+
+/*
+ * fp8_gemm_gated_grad -- its backward pass: the gradient of the block's inner product, and out of it those of both projections:
+ *     c = (op(A) op(B)) / (sA * sB);  y = [c * u * act'(g) | c * act(g)],  [g | u] = GU
+ *     dGU = cast_out(y), or encode(fl32(y * sD)) for FP8 kinds;  amax = max |y|
+ *   A, B  the gradient of the block's output (M x K) and the down projection's weight (op(B): K x F)
+ *   GU    device, M x 2F of GU_dtype, as fp8_gemm_gated kept it; may be dGU itself where the types are the same
+ *   dGU   device, M x 2F of out_kind: operand of the products for the input's gradient (times the weights [2F, in]) and theirs
+ * The rest as for fp8_gemm_act.
+ */
+int fp8_gemm_gated_grad(const uint8_t* A, int fmtA, int transA, const uint8_t* B, int fmtB, int transB,
+                        void* dGU, int out_kind, int64_t M, int64_t F, int64_t K,
+                        const float* sA_dev, int64_t nsA, const float* sB_dev, int64_t nsB, int act,
+                        const void* GU, int GU_dtype, const float* sD_dev, float* amax_out, int flags, void* stream);
+
+/*
+ * fp8_grad_norm, fp8_grad_clip -- the global norm of `count` gradient tensors and their clipping to it:
+ *     norm = sqrt(sum over all tensors and elements of x^2);   out = cast(x * min(1, max_norm / (norm + 1e-6)))
+ * x, n, dtype and out are HOST arrays of `count` entries (read before the call returns); x[i] is a device pointer to n[i]
+ * contiguous elements of dtype[i] (fp8_dtype_t), which may start anywhere its element may.
+ *   norm_out   device, one fp32.  Squares are added in 64 bits, in the same order in every run.
+ *   workspace  device, 8-byte aligned, FP8_GRAD_NORM_WORKSPACE_BYTES bytes, zero-filled once before its first use; calls
+ *              that may overlap need workspaces of their own
+ *   out        out[i] has x[i]'s type; NULL, or out[i] = x[i]: in place.  Other overlaps are not allowed.
+ *   norm       device, one fp32 (what fp8_grad_norm wrote)
+ *   max_norm   a number >= 0
+ * An infinite norm makes the factor 0, a NaN norm makes every output NaN.  Tensors of no elements may have NULL pointers.
+ */
+#define FP8_GRAD_NORM_WORKSPACE_BYTES 32768
+int fp8_grad_norm(int count, const void* const* x, const size_t* n, const int* dtype, float* norm_out, void* workspace, void* stream);
+int fp8_grad_clip(int count, const void* const* x, const size_t* n, const int* dtype, void* const* out, const float* norm,
+                  float max_norm, void* stream);
 
 /*
  * Which kernel the GEMM entry points would run for a problem, small ones apart (diagnostics; nothing is launched and

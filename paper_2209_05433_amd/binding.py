@@ -18,6 +18,8 @@ FP8_AMAX_WORKSPACE_BYTES = 16384
 FP8_SPLITK_STATIC_BYTES = 64 << 20
 FP8_GEMM_MFMA8 = 1
 FP8_OUT_F32, FP8_OUT_BF16, FP8_OUT_E4M3, FP8_OUT_E5M2 = 0, 1, 2, 3
+FP8_ACT_NONE, FP8_ACT_RELU, FP8_ACT_GELU, FP8_ACT_GELU_TANH, FP8_ACT_SILU = range(5)
+FP8_GRAD_NORM_WORKSPACE_BYTES = 32768
 FP8_PLAN_NO_GEMM, FP8_PLAN_FMA_KERNEL, FP8_PLAN_TILED_256x256, FP8_PLAN_TILED_256x128, FP8_PLAN_MFMA_ANY, FP8_PLAN_TILED_MIXED = 0, 1, 2, 3, 4, 5
 FP8_PLAN_ELEMENTWISE_STORES = 16
 FP8_MULTI_MAX = 4
@@ -35,7 +37,8 @@ EXPORTS = (
     "fp8_quantize_dscale", "fp8_quantize_ex", "fp8_dequantize", "fp8_quantize_amax", "fp8_quantize_sr",
     "fp8_scale_from_amax_history", "fp8_scale_from_amax_n", "fp8_amax_rows", "fp8_quantize_rows",
     "fp8_quantize_transpose", "fp8_gemm", "fp8_gemm_dscale", "fp8_gemm_mfma8",
-    "fp8_gemm_mfma8_dscale", "fp8_gemm_ex", "fp8_gemm_splitk", "fp8_gemm_splitk_workspace_size", "fp8_gemm_splitk_static", "fp8_gemm_fused", "fp8_scaled_gemm", "fp8_gemm_plan", "fp8_gemm_form", "fp8_set_knob", "fp8_get_knob",
+    "fp8_gemm_mfma8_dscale", "fp8_gemm_ex", "fp8_gemm_splitk", "fp8_gemm_splitk_workspace_size", "fp8_gemm_splitk_static", "fp8_gemm_fused", "fp8_scaled_gemm",
+    "fp8_gemm_act", "fp8_gemm_act_grad", "fp8_gemm_act_grad_workspace_size", "fp8_gemm_gated", "fp8_gemm_gated_grad", "fp8_grad_norm", "fp8_grad_clip", "fp8_gemm_plan", "fp8_gemm_form", "fp8_set_knob", "fp8_get_knob",
     "fp8_last_error", "fp8_version",
 )
 
@@ -80,6 +83,13 @@ def lib() -> ctypes.CDLL:
     L.fp8_gemm_splitk_static.argtypes, L.fp8_gemm_splitk_static.restype = [vp, i, i, vp, i, i, vp, i64, i64, i64, i, f, f, vp, vp, i, i, vp], i
     L.fp8_gemm_splitk_workspace_size.argtypes, L.fp8_gemm_splitk_workspace_size.restype = [i64, i64, i64, i, i, i], sz
     L.fp8_gemm_fused.argtypes, L.fp8_gemm_fused.restype = [vp, i, i, vp, i, i, vp, i, i64, i64, i64, vp, i64, vp, i64, vp, vp, i, vp], i
+    L.fp8_gemm_act.argtypes, L.fp8_gemm_act.restype = [vp, i, i, vp, i, i, vp, i, i64, i64, i64, vp, i64, vp, i64, i, vp, i, vp, i, vp, i, vp, vp, i, vp], i
+    L.fp8_gemm_act_grad.argtypes, L.fp8_gemm_act_grad.restype = [vp, i, i, vp, i, i, vp, i, i64, i64, i64, vp, i64, vp, i64, i, vp, i, vp, vp, sz, vp, vp, i, vp], i
+    L.fp8_gemm_act_grad_workspace_size.argtypes, L.fp8_gemm_act_grad_workspace_size.restype = [i64, i64], sz
+    L.fp8_gemm_gated.argtypes, L.fp8_gemm_gated.restype = [vp, i, i, vp, i, i, vp, i, i64, i64, i64, vp, i64, vp, i64, i, vp, i, vp, vp, i, vp], i
+    L.fp8_gemm_gated_grad.argtypes, L.fp8_gemm_gated_grad.restype = L.fp8_gemm_gated.argtypes, i
+    L.fp8_grad_norm.argtypes, L.fp8_grad_norm.restype = [i, vp, vp, vp, vp, vp, vp], i
+    L.fp8_grad_clip.argtypes, L.fp8_grad_clip.restype = [i, vp, vp, vp, vp, vp, f, vp], i
     L.fp8_quantize_sr.argtypes, L.fp8_quantize_sr.restype = [vp, sz, i, i, f, vp, c.c_uint64, vp, vp], i
     L.fp8_quantize_amax.argtypes, L.fp8_quantize_amax.restype = [vp, sz, i, i, vp, vp, vp, vp], i
     L.fp8_scale_from_amax_history.argtypes, L.fp8_scale_from_amax_history.restype = [vp, sz, i, vp, vp], i
@@ -159,6 +169,11 @@ def fp8_gemm_splitk_workspace_size(M: int, N: int, K: int, transA: bool, transB:
     return int(lib().fp8_gemm_splitk_workspace_size(M, N, K, int(bool(transA)), int(bool(transB)), int(splits)))
 
 
+def fp8_gemm_act_grad_workspace_size(M: int, N: int) -> int:
+    """Bytes of the workspace that fp8_gemm_act_grad needs for the bias gradient of an M x N output."""
+    return int(lib().fp8_gemm_act_grad_workspace_size(M, N))
+
+
 # The entry points that take tensors: unpacked in C (csrc/native_binding.cpp; their argument names and
 # defaults are in the docstrings there), since marshalling them here costs more than a short launch.
 TENSOR_CALLS = (
@@ -166,6 +181,7 @@ TENSOR_CALLS = (
     "fp8_quantize_ex", "fp8_dequantize", "fp8_quantize_amax", "fp8_quantize_sr", "fp8_scale_from_amax_history", "fp8_scale_from_amax_n",
     "fp8_amax_rows", "fp8_quantize_rows", "fp8_quantize_transpose", "fp8_gemm", "fp8_gemm_dscale", "fp8_gemm_mfma8", "fp8_gemm_mfma8_dscale",
     "fp8_gemm_ex", "fp8_gemm_splitk", "fp8_gemm_splitk_static", "fp8_gemm_fused", "fp8_scaled_gemm",
+    "fp8_gemm_act", "fp8_gemm_act_grad", "fp8_gemm_gated", "fp8_gemm_gated_grad", "fp8_grad_norm", "fp8_grad_clip",
 )
 
 _native = None

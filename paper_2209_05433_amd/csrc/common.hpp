@@ -78,5 +78,8 @@ int launch_quantize_transpose(const void* x, int64_t rows, int64_t cols, int in_
                               uint8_t* q_out, uint8_t* qt_out, hipStream_t stream);
 int launch_dequantize(const uint8_t* q, size_t n, int fmt, float scale, const float* scale_dev,
                       int out_dtype, void* out, hipStream_t stream);
+int launch_grad_norm(int count, const void* const* x, const size_t* n, const int* dtype, float* norm_out, void* workspace, hipStream_t stream);
+int launch_grad_clip(int count, const void* const* x, const size_t* n, const int* dtype, void* const* out, const float* norm, float max_norm,
+                     hipStream_t stream);
 
 }  // namespace fp8mm

@@ -1,0 +1,153 @@
+// Products with an operator behind them (gemm_op.hpp): which kernel takes a call, the kernel of plain FMAs that takes any, and the sum
+// of the partial column sums (gfx950).
+#include "gemm_op.hpp"
+
+namespace fp8mm {
+namespace {
+
+// ------------------------------------------------------------------------------------------
+// Any shape, any alignment, every storage order: 64 x 64 outputs per workgroup of 256, 4 x 4 per thread, operands decoded to
+// 32 bits (exactly) on their way into LDS, 32-bit FMAs.  The cross-check of the matrix-core forms, and what is left for the calls that they
+// do not take.
+// ------------------------------------------------------------------------------------------
+constexpr int GT = 64, GK = 16;
+
+template <int FMT_A, int FMT_B, bool PAIR>
+__global__ __launch_bounds__(256) void gemm_op_generic_kernel(const uint8_t* __restrict__ A, const uint8_t* __restrict__ B, void* D,
+                                                              int64_t M, int64_t N, int64_t K, OpArgs o, bool transA, bool transB)
+{
+    constexpr int P = PAIR ? 2 : 1;
+    __shared__ float As[GK][GT + 1];
+    __shared__ float Bs[P][GK][GT + 1];
+    __shared__ float sums[16][GT];
+    const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+    const int64_t tiles_n = (N + GT - 1) / GT;
+    const int64_t tm = blockIdx.x / tiles_n, m0 = tm * GT, n0 = (int64_t)(blockIdx.x % tiles_n) * GT;
+    float acc[P][4][4] = {};
+    for (int64_t k0 = 0; k0 < K; k0 += GK) {
+        for (int e = tid; e < GT * GK; e += 256) {
+            const int r = transA ? e % GT : e / GK, kk = transA ? e / GT : e % GK;      // consecutive lanes along the rows in memory
+            const int64_t gm = m0 + r, gk = k0 + kk;
+            As[kk][r] = gm < M && gk < K ? decode_fp8<FMT_A>(A[transA ? gk * M + gm : gm * K + gk]) : 0.0f;
+        }
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+            for (int e = tid; e < GT * GK; e += 256) {
+                const int r = transB ? e / GK : e % GT, kk = transB ? e % GK : e / GT;
+                const int64_t gn = n0 + r, gk = k0 + kk, at = gn + p * N;
+                Bs[p][kk][r] = gn < N && gk < K ? decode_fp8<FMT_B>(B[transB ? at * K + gk : gk * (P * N) + at]) : 0.0f;
+            }
+        __syncthreads();
+#pragma unroll
+        for (int kk = 0; kk < GK; ++kk)
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[p][i][j] = __builtin_fmaf(As[kk][ty * 4 + i], Bs[p][kk][tx * 4 + j], acc[p][i][j]);
+        __syncthreads();
+    }
+    const float sD = o.out_kind >= OUT_E4M3 ? scale_value(o.sD_dev, 1.0f) : 1.0f;
+    const int64_t col = n0 + tx * 4;
+    const int left = col < N ? (int)(N - col < 4 ? N - col : 4) : 0;
+    unsigned top = 0;
+    float total[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (left > 0) {
+        float bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (o.bias) load_row<4>(o.bias, o.bias_dtype, col, left, bias);
+        double fy[4], fu[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int64_t c = j < left ? col + j : col;
+            fy[j] = op_column_factor(o, N, c, false);
+            fu[j] = PAIR ? op_column_factor(o, N, c, true) : 0.0;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t row = m0 + ty * 4 + i;
+            if (row >= M) continue;
+            const double a = 1.0 / (double)o.sA_dev[o.a_per_row ? row : 0];
+            float y[4], u[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                y[j] = acc[0][i][j] * (float)(a * fy[j]);
+                u[j] = PAIR ? acc[P - 1][i][j] * (float)(a * fu[j]) : 0.0f;
+            }
+            top = max(top, op_row<4>(o, D, N, row, col, left, y, u, bias, sD));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) total[j] += y[j];
+        }
+    }
+    if (o.sums) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sums[ty][tx * 4 + j] = total[j];
+        __syncthreads();
+        if (tid < GT && n0 + tid < N) {
+            float s = 0.0f;
+            for (int i = 0; i < 16; ++i) s += sums[i][tid];
+            o.sums[tm * N + n0 + tid] = s;
+        }
+    }
+    if (o.amax_out) wave_amax_commit(top, o.amax_out);
+}
+
+template <int FA, int FB>
+void enqueue_generic(const GemmArgs& g, const OpArgs& o, unsigned tiles)
+{
+    if (op_pair_in(o.op)) enqueue(gemm_op_generic_kernel<FA, FB, true>, dim3(tiles), dim3(256), 0, g.stream, g.A, g.B, g.C, g.M, g.N, g.K, o, g.transA, g.transB);
+    else enqueue(gemm_op_generic_kernel<FA, FB, false>, dim3(tiles), dim3(256), 0, g.stream, g.A, g.B, g.C, g.M, g.N, g.K, o, g.transA, g.transB);
+}
+
+int launch_generic(const GemmArgs& g, const OpArgs& o, int64_t& parts)
+{
+    const int64_t tiles = ((g.M + GT - 1) / GT) * ((g.N + GT - 1) / GT);
+    if (tiles > 0x7fffffffll) return fail(FP8_ERR_UNSUPPORTED, "gemm with an operator: %lld tiles of 64 x 64 exceed the grid limit", (long long)tiles);
+    parts = (g.M + GT - 1) / GT;
+    if (g.fmtA == FP8_E4M3) {
+        if (g.fmtB == FP8_E4M3) enqueue_generic<FP8_E4M3, FP8_E4M3>(g, o, (unsigned)tiles);
+        else enqueue_generic<FP8_E4M3, FP8_E5M2>(g, o, (unsigned)tiles);
+    } else {
+        if (g.fmtB == FP8_E4M3) enqueue_generic<FP8_E5M2, FP8_E4M3>(g, o, (unsigned)tiles);
+        else enqueue_generic<FP8_E5M2, FP8_E5M2>(g, o, (unsigned)tiles);
+    }
+    return check_launch("gemm with an operator (plain FMAs)");
+}
+
+__global__ void op_zero_cell_kernel(unsigned* p) { *p = 0u; }
+
+// dbias_j = sum of the rows of partial sums, always in the same order: a workgroup of 4 waves takes 64 columns, wave w the rows w, w + 4, ...
+// No rows: zeros.
+__global__ __launch_bounds__(256) void column_sum_kernel(const float* __restrict__ sums, int64_t parts, int64_t N, float* __restrict__ dbias)
+{
+    __shared__ float part[4][64];
+    const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int64_t col = (int64_t)blockIdx.x * 64 + l;
+    float s = 0.0f;
+    if (col < N)
+        for (int64_t i = w; i < parts; i += 4) s += sums[i * N + col];
+    part[w][l] = s;
+    __syncthreads();
+    if (w == 0 && col < N) dbias[col] = (part[0][l] + part[1][l]) + (part[2][l] + part[3][l]);
+}
+
+}  // namespace
+
+int launch_gemm_op(const GemmArgs& g, const OpArgs& o, float* dbias)
+{
+    if (dbias && g.N > (int64_t)0x7fffffff * 64) return fail(FP8_ERR_UNSUPPORTED, "gemm with an operator: dbias of %lld values exceeds the grid limit", (long long)g.N);
+    if (o.amax_out) {                                        // written, not accumulated
+        enqueue(op_zero_cell_kernel, dim3(1), dim3(1), 0, g.stream, (unsigned*)o.amax_out);
+        if (int e = check_launch("gemm with an operator (amax init)")) return e;
+    }
+    int64_t parts = 0;
+    if (g.M > 0 && g.N > 0)
+        if (int e = launch_generic(g, o, parts)) return e;
+    if (dbias && g.N > 0) {
+        enqueue(column_sum_kernel, dim3((unsigned)((g.N + 63) / 64)), dim3(256), 0, g.stream, o.sums, parts, g.N, dbias);
+        return check_launch("gemm with an operator (column sums)");
+    }
+    return FP8_OK;
+}
+
+}  // namespace fp8mm

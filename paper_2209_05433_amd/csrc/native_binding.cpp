@@ -14,6 +14,8 @@
 #include <stdio.h>
 #include <string.h>
 
+#include <vector>
+
 #include "fp8mm.h"
 
 namespace {
@@ -599,6 +601,158 @@ ENTRY(fp8_scaled_gemm, 12, "a", "fmtA", "transA", "b", "fmtB", "transB", "qa_out
     return checked([&] { return ::fp8_scaled_gemm(p.A, p.B, dt, tA, tB, p.M, p.N, p.K, fa, fb, qa, qb, amax, scale, w, p.C, odt, flags, s); });
 }
 
+// ---- products with an operator behind them ---------------------------------------------------------------
+// What the four have in common: operands, output, factors.  pair_in: op(B) has two columns for each output column; pair_out: the output
+// has two for each of op(B).
+struct OpProduct {
+    const uint8_t *A, *B;
+    void *D, *stream;
+    const float *sA, *sB, *sD;
+    float* amax;
+    int64_t M, N, K, nA, nB;
+    int fa, fb, tA, tB, kind, act, flags;
+    OpProduct(const Args& a, bool pair_in, bool pair_out, int at_sD, const char* output, const char* shapes)
+    {
+        const at::Tensor &ta = tensor(a[0], "A"), &tb = tensor(a[3], "B"), &d = tensor(a[6], output), &fA = tensor(a[8], "sA"), &fB = tensor(a[9], "sB");
+        tA = truth(a[2]); tB = truth(a[5]); kind = small_of_int(a[7]);
+        if (ta.dim() != 2 || tb.dim() != 2 || !is_bytes(ta) || !is_bytes(tb)) raise(PyExc_ValueError, "%s", kBytes2d);
+        M = ta.size(tA ? 1 : 0); K = ta.size(tA ? 0 : 1);
+        const int64_t columns = tb.size(tB ? 0 : 1);
+        N = pair_in ? columns / 2 : columns;
+        if (tb.size(tB ? 1 : 0) != K || (pair_in && columns % 2) || !has_shape(d, M, pair_out ? 2 * N : N)) raise(PyExc_ValueError, "%s", shapes);
+        const at::ScalarType want = kind == FP8_OUT_F32 ? at::kFloat : kind == FP8_OUT_BF16 ? at::kBFloat16 : at::kByte;
+        if (d.scalar_type() != want) {
+            PyErr_Format(PyExc_ValueError, "%s must be %s for out_kind %d", output, c10::toString(want), kind);
+            throw Failed{};
+        }
+        if (fA.scalar_type() != at::kFloat || fB.scalar_type() != at::kFloat) raise(PyExc_ValueError, "sA and sB must be fp32 device tensors");
+        A = (const uint8_t*)device_or_null(ta, "A"); B = (const uint8_t*)device_or_null(tb, "B");
+        D = written_or_null(d, output);
+        sA = (const float*)device(fA, "sA"); sB = (const float*)device(fB, "sB");
+        nA = fA.numel(); nB = fB.numel();
+        sD = is_none(a[at_sD]) ? nullptr : cells(a[at_sD], "the output's factor", 1);
+        amax = is_none(a[at_sD + 1]) ? nullptr : cells_out(a[at_sD + 1], "amax_out", 1);
+        fa = small(a[1]); fb = small(a[4]); act = small_of_int(a[10]); flags = small_of_int(a[at_sD + 2]);
+        stream = stream_of(a[at_sD + 3]);
+    }
+    // A tensor beside the product, of the given number of columns (rows < 0: a vector), or None.
+    const at::Tensor* side(PyObject* o, const char* what, int64_t rows, int64_t columns, bool required = false) const
+    {
+        if (is_none(o)) {
+            if (required) raise(PyExc_TypeError, "%s must be a tensor", what);
+            return nullptr;
+        }
+        const at::Tensor& t = tensor(o, what);
+        if (rows < 0 ? t.dim() != 1 || t.size(0) != columns : !has_shape(t, rows, columns)) raise(PyExc_ValueError, "%s does not have the shape that belongs to the product", what);
+        return &t;
+    }
+};
+const void* read_of(const at::Tensor* t, const char* what) { return t ? device_or_null(*t, what) : nullptr; }
+void* written_of(const at::Tensor* t, const char* what) { return t ? written_or_null(*t, what) : nullptr; }
+int type_of(const at::Tensor* t) { return t ? dtype_of(*t) : FP8_F32; }
+
+ENTRY(fp8_gemm_act, 11, "A", "fmtA", "transA", "B", "fmtB", "transB", "D", "out_kind", "sA", "sB", "act", "bias", "residual", "Z", "sD", "amax_out", "flags", "stream")
+{
+    const OpProduct p(a, false, false, 14, "D", "shapes do not form D[M,N] = op(A)[M,K] op(B)[K,N]");
+    const at::Tensor *bias = p.side(a[11], "bias", -1, p.N), *res = p.side(a[12], "residual", p.M, p.N), *z = p.side(a[13], "Z", p.M, p.N);
+    const void *pb = read_of(bias, "bias"), *pr = read_of(res, "residual");
+    void* pz = written_of(z, "Z");
+    const int tb = type_of(bias), tr = type_of(res), tz = type_of(z);
+    return checked([&] { return ::fp8_gemm_act(p.A, p.fa, p.tA, p.B, p.fb, p.tB, p.D, p.kind, p.M, p.N, p.K, p.sA, p.nA, p.sB, p.nB, p.act, pb, tb, pr, tr, pz, tz,
+                                               p.sD, p.amax, p.flags, p.stream); });
+}
+
+ENTRY(fp8_gemm_act_grad, 12, "A", "fmtA", "transA", "B", "fmtB", "transB", "D", "out_kind", "sA", "sB", "act", "Z", "dbias", "workspace", "sD", "amax_out", "flags", "stream")
+{
+    const OpProduct p(a, false, false, 14, "D", "shapes do not form D[M,N] = op(A)[M,K] op(B)[K,N]");
+    const at::Tensor* z = p.side(a[11], "Z", p.M, p.N, true);
+    const void* pz = read_of(z, "Z");
+    const int tz = type_of(z);
+    float* db = is_none(a[12]) ? nullptr : cells_out(a[12], "dbias", p.N);
+    if (db && p.N == 0) db = nullptr;
+    void* ws = nullptr;
+    size_t bytes = 0;
+    if (!is_none(a[13])) {
+        const at::Tensor& w = tensor(a[13], "workspace");
+        ws = written_or_null(w, "workspace");
+        bytes = (size_t)w.numel() * w.element_size();
+    }
+    return checked([&] { return ::fp8_gemm_act_grad(p.A, p.fa, p.tA, p.B, p.fb, p.tB, p.D, p.kind, p.M, p.N, p.K, p.sA, p.nA, p.sB, p.nB, p.act, pz, tz, db, ws, bytes,
+                                                    p.sD, p.amax, p.flags, p.stream); });
+}
+
+ENTRY(fp8_gemm_gated, 11, "A", "fmtA", "transA", "B", "fmtB", "transB", "H", "out_kind", "sA", "sB", "act", "GU", "sH", "amax_out", "flags", "stream")
+{
+    const OpProduct p(a, true, false, 12, "H", "shapes do not form H[M,F] out of op(A)[M,K] op(B)[K,2F]");
+    const at::Tensor* gu = p.side(a[11], "GU", p.M, 2 * p.N);
+    void* pg = written_of(gu, "GU");
+    const int tg = type_of(gu);
+    return checked([&] { return ::fp8_gemm_gated(p.A, p.fa, p.tA, p.B, p.fb, p.tB, p.D, p.kind, p.M, p.N, p.K, p.sA, p.nA, p.sB, p.nB, p.act, pg, tg,
+                                                 p.sD, p.amax, p.flags, p.stream); });
+}
+
+ENTRY(fp8_gemm_gated_grad, 12, "A", "fmtA", "transA", "B", "fmtB", "transB", "dGU", "out_kind", "sA", "sB", "act", "GU", "sD", "amax_out", "flags", "stream")
+{
+    const OpProduct p(a, false, true, 12, "dGU", "shapes do not form dGU[M,2F] out of op(A)[M,K] op(B)[K,F]");
+    const at::Tensor* gu = p.side(a[11], "GU", p.M, 2 * p.N, true);
+    const void* pg = read_of(gu, "GU");
+    const int tg = type_of(gu);
+    return checked([&] { return ::fp8_gemm_gated_grad(p.A, p.fa, p.tA, p.B, p.fb, p.tB, p.D, p.kind, p.M, p.N, p.K, p.sA, p.nA, p.sB, p.nB, p.act, pg, tg,
+                                                      p.sD, p.amax, p.flags, p.stream); });
+}
+
+// The host arrays of the gradient calls.
+struct Gradients {
+    std::vector<const void*> x;
+    std::vector<size_t> n;
+    std::vector<int> dtype;
+    explicit Gradients(const Sequence& xs)
+    {
+        const Py_ssize_t count = xs.size();
+        x.reserve(count); n.reserve(count); dtype.reserve(count);
+        for (Py_ssize_t i = 0; i < count; ++i) {
+            const at::Tensor& t = tensor(xs[i], "x");
+            x.push_back(device_or_null(t, "x"));
+            n.push_back((size_t)t.numel());
+            dtype.push_back(dtype_of(t));
+        }
+    }
+};
+
+ENTRY(fp8_grad_norm, 3, "xs", "norm_out", "workspace", "stream")
+{
+    const Sequence xs(a[0], "xs must be a sequence of tensors");
+    const Gradients g(xs);
+    float* out = cells_out(a[1], "norm_out", 1);
+    const at::Tensor& ws = tensor(a[2], "workspace");
+    if (ws.numel() * (int64_t)ws.element_size() < FP8_GRAD_NORM_WORKSPACE_BYTES) raise(PyExc_ValueError, "workspace must hold FP8_GRAD_NORM_WORKSPACE_BYTES bytes");
+    void *w = written(ws, "workspace"), *s = stream_of(a[3]);
+    return checked([&] { return ::fp8_grad_norm((int)g.x.size(), g.x.data(), g.n.data(), g.dtype.data(), out, w, s); });
+}
+
+ENTRY(fp8_grad_clip, 3, "xs", "norm", "max_norm", "outs", "stream")
+{
+    const Sequence xs(a[0], "xs must be a sequence of tensors");
+    const float* norm = cells(a[1], "norm", 1);
+    const float most = real(a[2]);
+    const Gradients g(xs);
+    std::vector<void*> out;
+    if (is_none(a[3])) {
+        for (Py_ssize_t i = 0; i < xs.size(); ++i) out.push_back(written_or_null(tensor(xs[i], "x"), "x"));     // (x itself is written)
+    } else {
+        const Sequence outs(a[3], "outs must be a sequence of tensors");
+        bool fine = outs.size() == xs.size();
+        for (Py_ssize_t i = 0; fine && i < outs.size(); ++i) {
+            const at::Tensor &t = tensor(outs[i], "out"), &x = tensor(xs[i], "x");
+            fine = t.scalar_type() == x.scalar_type() && t.numel() == x.numel();
+            if (fine) out.push_back(written_or_null(t, "out"));
+        }
+        if (!fine) raise(PyExc_ValueError, "outs must be tensors of the types and element counts of xs");
+    }
+    void* s = stream_of(a[4]);
+    return checked([&] { return ::fp8_grad_clip((int)g.x.size(), g.x.data(), g.n.data(), g.dtype.data(), out.data(), norm, most, s); });
+}
+
 // Called once by the package: the exception that failing calls raise.
 PyObject* py_set_error(PyObject*, PyObject* type)
 {
@@ -647,6 +801,20 @@ PyMethodDef methods[] = {
            "cast of both operands and their FP8 product in one call.  a is [M, K] (or\n[K, M] if transA), b is [K, N] (or [N, K] if transB), both bf16 or both fp32; "
            "qa_out / qb_out are\nuint8 tensors of the operands' shapes; amax_out and scale_out hold two floats ([0]: a, [1]: b);\nworkspace: 2 * FP8_AMAX_WORKSPACE_BYTES "
            "bytes, zero-filled once."),
+    METHOD(fp8_gemm_act, "fp8_gemm_act(A, fmtA, transA, B, fmtB, transB, D, out_kind, sA, sB, act, bias=None, residual=None, Z=None, sD=None, amax_out=None, flags=0, "
+           "stream=None)\n--\n\nD = act(op(A) op(B) / (sA sB) + bias) + residual.  A, B, D, factors and flags as for fp8_gemm_fused; bias [N],\nresidual [M, N] (may be D itself) "
+           "and Z [M, N] (receives the value before the activation) are float32 or bfloat16."),
+    METHOD(fp8_gemm_act_grad, "fp8_gemm_act_grad(A, fmtA, transA, B, fmtB, transB, D, out_kind, sA, sB, act, Z, dbias=None, workspace=None, sD=None, amax_out=None, flags=0, "
+           "stream=None)\n--\n\nD = op(A) op(B) / (sA sB) * act'(Z); dbias: None or N fp32 values that receive the column sums of D, with a\nworkspace (any dtype) of at least "
+           "fp8_gemm_act_grad_workspace_size(M, N) bytes."),
+    METHOD(fp8_gemm_gated, "fp8_gemm_gated(A, fmtA, transA, B, fmtB, transB, H, out_kind, sA, sB, act, GU=None, sH=None, amax_out=None, flags=0, stream=None)\n--\n\n"
+           "H [M, F] = act(g) * u with [g | u] = op(A) op(B) / (sA sB); B is [2F, K] if transB, else [K, 2F], the gate first;\nsB: 1, 2 or 2F values; GU [M, 2F], float32 or "
+           "bfloat16, receives [g | u]."),
+    METHOD(fp8_gemm_gated_grad, "fp8_gemm_gated_grad(A, fmtA, transA, B, fmtB, transB, dGU, out_kind, sA, sB, act, GU, sD=None, amax_out=None, flags=0, stream=None)\n--\n\n"
+           "dGU [M, 2F] = [c u act'(g) | c act(g)] with c = op(A) op(B) / (sA sB) and [g | u] = GU."),
+    METHOD(fp8_grad_norm, "fp8_grad_norm(xs, norm_out, workspace, stream=None)\n--\n\nnorm_out (one fp32 value) = the 2-norm over all tensors of xs (float32 or bfloat16, mixed); workspace: "
+           "device tensor\nof at least FP8_GRAD_NORM_WORKSPACE_BYTES bytes, zero-filled once before its first use."),
+    METHOD(fp8_grad_clip, "fp8_grad_clip(xs, norm, max_norm, outs=None, stream=None)\n--\n\nouts = xs * min(1, max_norm / (norm + 1e-6)), in place where outs is None."),
     {"set_error", py_set_error, METH_O, "The exception class that failing calls raise."},
     {nullptr, nullptr, 0, nullptr}};
 
