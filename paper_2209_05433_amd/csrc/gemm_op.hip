@@ -74,7 +74,7 @@ __global__ __launch_bounds__(256) void gemm_op_generic_kernel(const uint8_t* __r
                 y[j] = acc[0][i][j] * (float)(a * fy[j]);
                 u[j] = PAIR ? acc[P - 1][i][j] * (float)(a * fu[j]) : 0.0f;
             }
-            top = max(top, op_row<4>(o, D, N, row, col, left, y, u, bias, sD));
+            top = max(top, op_row<4, PAIR>(o, D, N, row, col, left, y, u, bias, sD));
 #pragma unroll
             for (int j = 0; j < 4; ++j) total[j] += y[j];
         }
@@ -131,7 +131,32 @@ __global__ __launch_bounds__(256) void column_sum_kernel(const float* __restrict
     if (w == 0 && col < N) dbias[col] = (part[0][l] + part[1][l]) + (part[2][l] + part[3][l]);
 }
 
+// Which matrix-core kernel takes the call, as for the plain product of the same operands; none: SMALL_NONE.
+int choose_form(const GemmArgs& g, const OpArgs& o)
+{
+    GemmArgs p = g;
+    if (op_pair_in(o.op)) p.N = 2 * g.N;
+    p.ep.out_kind = o.out_kind; p.ep.sA_dev = o.sA_dev; p.ep.sB_dev = o.sB_dev; p.ep.amax_out = o.amax_out;
+    p.ep.a_per_row = o.a_per_row; p.ep.b_per_col = o.b_factors != B_ONE;
+    const GemmPlan plan = plan_gemm(p, false);
+    if (plan.kernel == GEMM_GENERIC || (op_pair_in(o.op) && !g.transB && g.N < 16)) return SMALL_NONE;
+    if (plan.small != SMALL_NONE) return plan.small;
+    return ((g.M + 63) / 64) * ((p.N + 63) / 64) <= 0x7fffffffll ? SMALL_64x64 : SMALL_NONE;
+}
+
 }  // namespace
+
+int raise_lds_limit(const void* kernel, int bytes, std::atomic<unsigned long long>& done)
+{
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess) return fail(FP8_ERR_DEVICE, "hipGetDevice failed");
+    const unsigned long long bit = 1ull << (dev & 63);
+    if (dev < 64 && (done.load(std::memory_order_relaxed) & bit)) return FP8_OK;
+    const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != hipSuccess) return fail(FP8_ERR_DEVICE, "hipFuncSetAttribute(LDS=%d): %s", bytes, hipGetErrorString(e));
+    if (dev < 64) done.fetch_or(bit, std::memory_order_relaxed);
+    return FP8_OK;
+}
 
 int launch_gemm_op(const GemmArgs& g, const OpArgs& o, float* dbias)
 {
@@ -141,8 +166,18 @@ int launch_gemm_op(const GemmArgs& g, const OpArgs& o, float* dbias)
         if (int e = check_launch("gemm with an operator (amax init)")) return e;
     }
     int64_t parts = 0;
-    if (g.M > 0 && g.N > 0)
-        if (int e = launch_generic(g, o, parts)) return e;
+    if (g.M > 0 && g.N > 0) {
+        const int form = g.K > 0 ? choose_form(g, o) : SMALL_NONE;
+        if (form == SMALL_NONE) {
+            if (int e = launch_generic(g, o, parts)) return e;
+        } else {
+            typedef int (*small_fn)(const GemmArgs&, const OpArgs&, int);
+            static const small_fn table[4] = {FP8MM_OP_SMALL_NAME(0), FP8MM_OP_SMALL_NAME(1), FP8MM_OP_SMALL_NAME(2), FP8MM_OP_SMALL_NAME(3)};
+            if (int e = table[(g.transA ? 2 : 0) + (g.transB ? 1 : 0)](g, o, form)) return e;
+            const int64_t rows = form == SMALL_32x32 || form == SMALL_32x64 ? 32 : 64;
+            parts = (g.M + rows - 1) / rows;
+        }
+    }
     if (dbias && g.N > 0) {
         enqueue(column_sum_kernel, dim3((unsigned)((g.N + 63) / 64)), dim3(256), 0, g.stream, o.sums, parts, g.N, dbias);
         return check_launch("gemm with an operator (column sums)");

@@ -14,6 +14,8 @@
 
 #include "gemm_common.hpp"
 
+#include <atomic>
+
 namespace fp8mm {
 
 enum { OP_ACT = 0, OP_ACT_GRAD = 1, OP_GATED = 2, OP_GATED_GRAD = 3 };
@@ -38,6 +40,18 @@ inline int64_t op_width(int op, int64_t N) { return op == OP_GATED_GRAD ? 2 * N 
 
 // g: operands, D, M, N (columns of D, or of either half), K; g.ep is not looked at.
 int launch_gemm_op(const GemmArgs& g, const OpArgs& o, float* dbias);
+
+// The kernel of small tiles (gemm_op_small.hip), one translation unit per pair of storage orders; form: SMALL_*, of the 64 x 64 ones
+// those of chunks of 128 where both operands are contiguous along K.  g.N >= 16 where op(B)'s column pairs are contiguous along N.
+#define FP8MM_OP_SMALL_NAME_(l) launch_op_small_l##l
+#define FP8MM_OP_SMALL_NAME(l) FP8MM_OP_SMALL_NAME_(l)
+int FP8MM_OP_SMALL_NAME(0)(const GemmArgs& g, const OpArgs& o, int form);
+int FP8MM_OP_SMALL_NAME(1)(const GemmArgs& g, const OpArgs& o, int form);
+int FP8MM_OP_SMALL_NAME(2)(const GemmArgs& g, const OpArgs& o, int form);
+int FP8MM_OP_SMALL_NAME(3)(const GemmArgs& g, const OpArgs& o, int form);
+
+// Raises a kernel's limit of dynamic LDS, once per device (`done`: of this kernel).
+int raise_lds_limit(const void* kernel, int bytes, std::atomic<unsigned long long>& done);
 
 namespace {
 
@@ -197,57 +211,53 @@ __device__ __forceinline__ unsigned max_bits_of(const float (&v)[W], int left)
 // ---- sums -> outputs ---------------------------------------------------------------------------------------------------
 // W columns from `col` on of row `row`, `left` (>= 1) of them inside; y, u: the values of c (u: of the second projection).  y is left as
 // what goes into the column sums (zeros outside).  Returns the largest |output| as bits.
-template <int W>
-__device__ __forceinline__ unsigned op_row(const OpArgs& o, void* D, int64_t N, int64_t row, int64_t col, int left, float (&y)[W], float (&u)[W],
+template <int W, bool PAIR>
+__device__ __forceinline__ unsigned op_row(const OpArgs& o, void* D, int64_t N, int64_t row, int64_t col, int left, float (&y)[W], const float (&u)[W],
                                            const float (&bias)[W], float sD)
 {
     float value[W], slope[W], side[W];
-    unsigned top;
-    switch (o.op) {
-        case OP_ACT:
-#pragma unroll
-            for (int i = 0; i < W; ++i) y[i] += bias[i];
-            if (o.kept) store_row<W>(o.kept, o.kept_dtype, row * N + col, left, y, 1.0f, 0);
-            act_row<W>(o.act, y, value, slope);
-            if (o.side) {
-                load_row<W>(o.side, o.side_dtype, row * N + col, left, side);
-#pragma unroll
-                for (int i = 0; i < W; ++i) value[i] += side[i];
-            }
-            top = max_bits_of<W>(value, left);
-            store_row<W>(D, o.out_kind, row * N + col, left, value, sD, top);
-            return top;
-        case OP_ACT_GRAD:
-            load_row<W>(o.side, o.side_dtype, row * N + col, left, side);
-            act_row<W>(o.act, side, value, slope);
-#pragma unroll
-            for (int i = 0; i < W; ++i) y[i] = i < left ? y[i] * slope[i] : 0.0f;
-            top = max_bits_of<W>(y, left);
-            store_row<W>(D, o.out_kind, row * N + col, left, y, sD, top);
-            return top;
-        case OP_GATED:
-            if (o.kept) {
-                store_row<W>(o.kept, o.kept_dtype, row * 2 * N + col, left, y, 1.0f, 0);
-                store_row<W>(o.kept, o.kept_dtype, row * 2 * N + N + col, left, u, 1.0f, 0);
-            }
-            act_row<W>(o.act, y, value, slope);
-#pragma unroll
-            for (int i = 0; i < W; ++i) value[i] *= u[i];
-            top = max_bits_of<W>(value, left);
-            store_row<W>(D, o.out_kind, row * N + col, left, value, sD, top);
-            return top;
-        default: {
-            load_row<W>(o.side, o.side_dtype, row * 2 * N + col, left, side);
-            act_row<W>(o.act, side, value, slope);
-            load_row<W>(o.side, o.side_dtype, row * 2 * N + N + col, left, side);
-#pragma unroll
-            for (int i = 0; i < W; ++i) { value[i] *= y[i]; y[i] *= side[i] * slope[i]; }
-            const unsigned top_y = max_bits_of<W>(y, left), top_u = max_bits_of<W>(value, left);
-            store_row<W>(D, o.out_kind, row * 2 * N + col, left, y, sD, top_y);
-            store_row<W>(D, o.out_kind, row * 2 * N + N + col, left, value, sD, top_u);
-            return max(top_y, top_u);
+    if (PAIR) {                                                           // OP_GATED
+        if (o.kept) {
+            store_row<W>(o.kept, o.kept_dtype, row * 2 * N + col, left, y, 1.0f, 0);
+            store_row<W>(o.kept, o.kept_dtype, row * 2 * N + N + col, left, u, 1.0f, 0);
         }
+        act_row<W>(o.act, y, value, slope);
+#pragma unroll
+        for (int i = 0; i < W; ++i) value[i] *= u[i];
+        const unsigned top = max_bits_of<W>(value, left);
+        store_row<W>(D, o.out_kind, row * N + col, left, value, sD, top);
+        return top;
     }
+    if (o.op == OP_ACT) {
+#pragma unroll
+        for (int i = 0; i < W; ++i) y[i] += bias[i];
+        if (o.kept) store_row<W>(o.kept, o.kept_dtype, row * N + col, left, y, 1.0f, 0);
+        act_row<W>(o.act, y, value, slope);
+        if (o.side) {
+            load_row<W>(o.side, o.side_dtype, row * N + col, left, side);
+#pragma unroll
+            for (int i = 0; i < W; ++i) value[i] += side[i];
+        }
+        const unsigned top = max_bits_of<W>(value, left);
+        store_row<W>(D, o.out_kind, row * N + col, left, value, sD, top);
+        return top;
+    }
+    const int64_t width = o.op == OP_GATED_GRAD ? 2 * N : N;
+    load_row<W>(o.side, o.side_dtype, row * width + col, left, side);
+    act_row<W>(o.act, side, value, slope);
+    unsigned top = 0;
+    if (o.op == OP_GATED_GRAD) {
+        load_row<W>(o.side, o.side_dtype, row * width + N + col, left, side);
+#pragma unroll
+        for (int i = 0; i < W; ++i) { value[i] *= y[i]; slope[i] *= side[i]; }
+        top = max_bits_of<W>(value, left);
+        store_row<W>(D, o.out_kind, row * width + N + col, left, value, sD, top);
+    }
+#pragma unroll
+    for (int i = 0; i < W; ++i) y[i] = i < left ? y[i] * slope[i] : 0.0f;
+    const unsigned top_y = max_bits_of<W>(y, left);
+    store_row<W>(D, o.out_kind, row * width + col, left, y, sD, top_y);
+    return max(top, top_y);
 }
 
 // 1 / the factor of a column of the product (up: of the second projection), in 64 bits: with 1 / sA it is rounded once.
