@@ -131,17 +131,28 @@ __global__ __launch_bounds__(256) void column_sum_kernel(const float* __restrict
     if (w == 0 && col < N) dbias[col] = (part[0][l] + part[1][l]) + (part[2][l] + part[3][l]);
 }
 
-// Which matrix-core kernel takes the call, as for the plain product of the same operands; none: SMALL_NONE.
-int choose_form(const GemmArgs& g, const OpArgs& o)
+// Which kernel takes the call, as for the plain product of the same operands.
+struct OpPlan { bool generic, tiled; int small, acc, tile_n; };
+OpPlan plan_op(const GemmArgs& g, const OpArgs& o)
 {
+    const bool pair = op_pair_in(o.op);
     GemmArgs p = g;
-    if (op_pair_in(o.op)) p.N = 2 * g.N;
-    p.ep.out_kind = o.out_kind; p.ep.sA_dev = o.sA_dev; p.ep.sB_dev = o.sB_dev; p.ep.amax_out = o.amax_out;
-    p.ep.a_per_row = o.a_per_row; p.ep.b_per_col = o.b_factors != B_ONE;
+    if (pair) p.N = 2 * g.N;
+    p.ep = o;
+    p.ep.b_per_col = o.b_factors != B_ONE;
+    if (g.K == 0 || (pair && !g.transB && g.N < 16)) return {true, false, SMALL_NONE, 0, 0};
     const GemmPlan plan = plan_gemm(p, false);
-    if (plan.kernel == GEMM_GENERIC || (op_pair_in(o.op) && !g.transB && g.N < 16)) return SMALL_NONE;
-    if (plan.small != SMALL_NONE) return plan.small;
-    return ((g.M + 63) / 64) * ((p.N + 63) / 64) <= 0x7fffffffll ? SMALL_64x64 : SMALL_NONE;
+    if (plan.kernel == GEMM_GENERIC) return {true, false, SMALL_NONE, 0, 0};
+    if (plan.small != SMALL_NONE) return {false, false, plan.small, g.acc, 0};
+    const bool tiled = plan.kernel != GEMM_MFMA_ANY && (!pair || (g.transB ? (uint64_t)(g.N + TILE_M) * (uint64_t)g.K < (1ull << 32) : g.N % 16 == 0));
+    if (!tiled) return {((g.M + 63) / 64) * ((p.N + 63) / 64) > 0x7fffffffll, false, SMALL_64x64, g.acc, 0};
+    // The width whose rounds of 256 workgroups take less time, as for the plain product.
+    const int acc = g.K % 16 ? (int)ACC_F16 : g.acc;
+    const TileTimes t = tile_times(acc, 2.0 * (double)((g.K + 2 * TILE_K - 1) / (2 * TILE_K)));
+    const int64_t tiles_m = (g.M + TILE_M - 1) / TILE_M;
+    auto rounds = [&](int64_t width) { return (double)((tiles_m * ((p.N + width - 1) / width) + 255) / 256); };
+    const int forced = knob(FP8_KNOB_TILE_N);
+    return {false, true, SMALL_NONE, acc, forced ? forced : rounds(128) * t.narrow < rounds(256) * t.wide ? 128 : 256};
 }
 
 }  // namespace
@@ -167,14 +178,20 @@ int launch_gemm_op(const GemmArgs& g, const OpArgs& o, float* dbias)
     }
     int64_t parts = 0;
     if (g.M > 0 && g.N > 0) {
-        const int form = g.K > 0 ? choose_form(g, o) : SMALL_NONE;
-        if (form == SMALL_NONE) {
+        typedef int (*small_fn)(const GemmArgs&, const OpArgs&, int);
+        static const small_fn small[4] = {FP8MM_OP_SMALL_NAME(0), FP8MM_OP_SMALL_NAME(1), FP8MM_OP_SMALL_NAME(2), FP8MM_OP_SMALL_NAME(3)};
+        typedef int (*tiled_fn)(const GemmArgs&, const OpArgs&);
+        static const tiled_fn tiled[4][2] = {{FP8MM_OP_TILED_NAME(0, 0), FP8MM_OP_TILED_NAME(0, 1)}, {FP8MM_OP_TILED_NAME(1, 0), FP8MM_OP_TILED_NAME(1, 1)},
+                                             {FP8MM_OP_TILED_NAME(2, 0), FP8MM_OP_TILED_NAME(2, 1)}, {FP8MM_OP_TILED_NAME(3, 0), FP8MM_OP_TILED_NAME(3, 1)}};
+        const int order = (g.transA ? 2 : 0) + (g.transB ? 1 : 0);
+        const OpPlan plan = plan_op(g, o);
+        if (plan.generic) {
             if (int e = launch_generic(g, o, parts)) return e;
         } else {
-            typedef int (*small_fn)(const GemmArgs&, const OpArgs&, int);
-            static const small_fn table[4] = {FP8MM_OP_SMALL_NAME(0), FP8MM_OP_SMALL_NAME(1), FP8MM_OP_SMALL_NAME(2), FP8MM_OP_SMALL_NAME(3)};
-            if (int e = table[(g.transA ? 2 : 0) + (g.transB ? 1 : 0)](g, o, form)) return e;
-            const int64_t rows = form == SMALL_32x32 || form == SMALL_32x64 ? 32 : 64;
+            GemmArgs p = g;
+            p.acc = plan.acc; p.tile_n = plan.tile_n;
+            if (int e = plan.tiled ? tiled[order][plan.acc == ACC_FP8 ? 1 : 0](p, o) : small[order](p, o, plan.small)) return e;
+            const int64_t rows = plan.tiled ? 128 : plan.small == SMALL_32x32 || plan.small == SMALL_32x64 ? 32 : 64;
             parts = (g.M + rows - 1) / rows;
         }
     }

@@ -22,16 +22,14 @@ enum { OP_ACT = 0, OP_ACT_GRAD = 1, OP_GATED = 2, OP_GATED_GRAD = 3 };
 // Factors of B: one; one of the gate's and one of the other projection's columns; one per column (2 N of them for OP_GATED).
 enum { B_ONE = 0, B_PAIR = 1, B_COLUMN = 2 };
 
-struct OpArgs {
-    const float *sA_dev, *sB_dev, *sD_dev;      // sD: null (= 1) or one value
-    float* amax_out;                            // null or one cell, zeroed by the launcher, raised with atomicMax
+struct OpArgs : EpilogueArgs {                  // (sA_dev, sB_dev: given; b_per_col: not looked at)
     float* sums;                                // null or partial column sums, a row of N for each kOpSumRows rows at least
     const void* bias;                           // null or N values
     const void* side;                           // residual (M x N or null), z (M x N), or g | u (M x 2 N)
     void* kept;                                 // null, z (M x N) or g | u (M x 2 N)
-    int op, act, out_kind;
+    int op, act;
     int bias_dtype, side_dtype, kept_dtype;     // fp8_dtype_t
-    int a_per_row, b_factors;
+    int b_factors;                              // B_*
 };
 
 constexpr int kOpSumRows = 32;                  // rows of the output behind one row of partial column sums, at least
@@ -49,6 +47,20 @@ int FP8MM_OP_SMALL_NAME(0)(const GemmArgs& g, const OpArgs& o, int form);
 int FP8MM_OP_SMALL_NAME(1)(const GemmArgs& g, const OpArgs& o, int form);
 int FP8MM_OP_SMALL_NAME(2)(const GemmArgs& g, const OpArgs& o, int form);
 int FP8MM_OP_SMALL_NAME(3)(const GemmArgs& g, const OpArgs& o, int form);
+
+// The tiled kernel (gemm_op_tiled.hip), one translation unit per (storage orders, accumulation mode); g.tile_n: 256 or 128 columns of
+// op(B).  The conditions of the plain product's tiled kernel, and for the gated block a second projection that begins on a 16-byte boundary less
+// than 2^32 bytes behind the first.
+#define FP8MM_OP_TILED_NAME_(l, a) launch_op_tiled_l##l##_a##a
+#define FP8MM_OP_TILED_NAME(l, a) FP8MM_OP_TILED_NAME_(l, a)
+#define FP8MM_DECLARE_OP_TILED(l) \
+    int FP8MM_OP_TILED_NAME(l, 0)(const GemmArgs& g, const OpArgs& o); \
+    int FP8MM_OP_TILED_NAME(l, 1)(const GemmArgs& g, const OpArgs& o);
+FP8MM_DECLARE_OP_TILED(0)
+FP8MM_DECLARE_OP_TILED(1)
+FP8MM_DECLARE_OP_TILED(2)
+FP8MM_DECLARE_OP_TILED(3)
+#undef FP8MM_DECLARE_OP_TILED
 
 // Raises a kernel's limit of dynamic LDS, once per device (`done`: of this kernel).
 int raise_lds_limit(const void* kernel, int bytes, std::atomic<unsigned long long>& done);
