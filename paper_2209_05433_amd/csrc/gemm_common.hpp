@@ -149,6 +149,8 @@ int fill_gemm_args(const char* who, GemmArgs& g, const uint8_t* A, int fmtA, int
 // 256 x 192 tile, fitted to 70 products so that it is taken where it is the faster one.
 struct TileTimes { double wide, middle, narrow; };
 TileTimes tile_times(int acc, double S);
+// Time until the last of Tw wide tiles (tw each) and then Tn narrow ones (tn each) ends on 256 units.
+double tiles_makespan(int64_t Tw, int64_t Tn, double tw, double tn);
 
 // ---- small device helpers used by the kernels -------------------------------------------------
 typedef u32x4 u32x4_any __attribute__((aligned(1)));     // 16 bytes at any address: one load or store on this target

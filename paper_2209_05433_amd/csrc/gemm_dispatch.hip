@@ -127,6 +127,23 @@ TileTimes tile_times(int acc, double S)
     return acc == ACC_FP8 ? TileTimes{0.62 * S + 8.9, 0.58 * S + 7.5, 0.46 * S + 5.2} : TileTimes{1.21 * S + 10.0, 1.03 * S + 7.6, 0.79 * S + 6.4};
 }
 
+double tiles_makespan(int64_t Tw, int64_t Tn, double tw, double tnar)
+{
+    const int64_t q = Tw / 256, k = Tw % 256;          // k units get q + 1 wide tiles, the others q
+    if (Tn == 0) return (double)(q + (k > 0)) * tw;
+    double best = 1e300;
+    for (int64_t r = 0; r <= Tn; ++r) {                // r narrow tiles on the units that are free first
+        const int64_t late = r * tnar >= tw ? (int64_t)((r * tnar - tw) / tnar) : 0;     // and as many as fit on the others
+        if ((256 - k) * r + k * late >= Tn) { best = std::max((double)(q + (k > 0)) * tw, (double)q * tw + (double)r * tnar); break; }
+    }
+    for (int64_t r = 1; r <= Tn; ++r) {                // or the last one ends on a unit that had q + 1 wide tiles
+        const int64_t early = (int64_t)((tw + r * tnar) / tnar);
+        if (k * r + (256 - k) * early >= Tn) { best = std::min(best, (double)(q + 1) * tw + (double)r * tnar); break; }
+        if ((double)(q + 1) * tw + (double)r * tnar >= best) break;
+    }
+    return best;
+}
+
 namespace {
 
 // Microseconds of the any-shape kernel in tiles of 256 x `width`: rounds of 256 tiles, each its ends (by output kind: fp32, bf16, FP8
@@ -305,23 +322,8 @@ GemmPlan plan_gemm(const GemmArgs& g, bool whole)
     // Knob FP8_KNOB_MIXED: 0 = by the model, 1 = never, 2 = wherever it is possible.
     const double S = 2.0 * (double)((K + 2 * TILE_K - 1) / (2 * TILE_K));
     double chosen_us = 1e300;
-    // time until the last of Tw wide tiles (tw us each) and then Tn narrow ones ends on 256 units
     const double tnar = tile.narrow;
-    auto makespan = [&](int64_t Tw, int64_t Tn, double tw) {
-        const int64_t q = Tw / 256, k = Tw % 256;          // k units get q + 1 wide tiles, the others q
-        if (Tn == 0) return (double)(q + (k > 0)) * tw;
-        double best = 1e300;
-        for (int64_t r = 0; r <= Tn; ++r) {                // r narrow tiles on the units that are free first
-            const int64_t late = r * tnar >= tw ? (int64_t)((r * tnar - tw) / tnar) : 0;     // and as many as fit on the others
-            if ((256 - k) * r + k * late >= Tn) { best = std::max((double)(q + (k > 0)) * tw, (double)q * tw + (double)r * tnar); break; }
-        }
-        for (int64_t r = 1; r <= Tn; ++r) {                // or the last one ends on a unit that had q + 1 wide tiles
-            const int64_t early = (int64_t)((tw + r * tnar) / tnar);
-            if (k * r + (256 - k) * early >= Tn) { best = std::min(best, (double)(q + 1) * tw + (double)r * tnar); break; }
-            if ((double)(q + 1) * tw + (double)r * tnar >= best) break;
-        }
-        return best;
-    };
+    auto makespan = [&](int64_t Tw, int64_t Tn, double tw) { return tiles_makespan(Tw, Tn, tw, tnar); };
     const bool few_rounds = plan.small == SMALL_NONE && g.splits <= 1 && tiles_m * wide_cols_all <= 64 * 256;
     if (few_rounds) chosen_us = std::min(makespan(tiles_m * wide_cols_all, 0, tile.wide), makespan(0, tiles_m * ((N + 127) / 128), tile.wide));
     if (!tn && mk != 1 && few_rounds && N > TILE_N) {

@@ -2,6 +2,8 @@
 // of the partial column sums (gfx950).
 #include "gemm_op.hpp"
 
+#include <algorithm>
+
 namespace fp8mm {
 namespace {
 
@@ -132,27 +134,42 @@ __global__ __launch_bounds__(256) void column_sum_kernel(const float* __restrict
 }
 
 // Which kernel takes the call, as for the plain product of the same operands.
-struct OpPlan { bool generic, tiled; int small, acc, tile_n; };
+struct OpPlan { bool generic, tiled; int small, acc, tile_n, wide_cols; };
 OpPlan plan_op(const GemmArgs& g, const OpArgs& o)
 {
     const bool pair = op_pair_in(o.op);
+    const OpPlan plain_fmas = {true, false, SMALL_NONE, 0, 0, 0};
     GemmArgs p = g;
     if (pair) p.N = 2 * g.N;
     p.ep = o;
     p.ep.b_per_col = o.b_factors != B_ONE;
-    if (g.K == 0 || (pair && !g.transB && g.N < 16)) return {true, false, SMALL_NONE, 0, 0};
+    if (g.K == 0 || (pair && !g.transB && g.N < 16)) return plain_fmas;
     const GemmPlan plan = plan_gemm(p, false);
-    if (plan.kernel == GEMM_GENERIC) return {true, false, SMALL_NONE, 0, 0};
-    if (plan.small != SMALL_NONE) return {false, false, plan.small, g.acc, 0};
-    const bool tiled = plan.kernel != GEMM_MFMA_ANY && (!pair || (g.transB ? (uint64_t)(g.N + TILE_M) * (uint64_t)g.K < (1ull << 32) : g.N % 16 == 0));
-    if (!tiled) return {((g.M + 63) / 64) * ((p.N + 63) / 64) > 0x7fffffffll, false, SMALL_64x64, g.acc, 0};
-    // The width whose rounds of 256 workgroups take less time, as for the plain product.
+    if (plan.kernel == GEMM_GENERIC) return plain_fmas;
+    if (plan.small != SMALL_NONE) return {false, false, plan.small, g.acc, 0, 0};
+    const bool tiled = plan.kernel != GEMM_MFMA_ANY && g.fmtB == FP8_E4M3 && (!pair || (g.transB ? (uint64_t)(g.N + TILE_M) * (uint64_t)g.K < (1ull << 32) : g.N % 16 == 0));
+    if (!tiled) return ((g.M + 63) / 64) * ((p.N + 63) / 64) > 0x7fffffffll ? plain_fmas : OpPlan{false, false, SMALL_64x64, g.acc, 0, 0};
+    // The width whose rounds of 256 workgroups take less time, or both widths in one launch, by the plain product's model of run times with the
+    // operator's own time on top (us of a 256-wide tile: fitted to 8192 x 8192 outputs over K = 256; it is the same per output in both widths).
     const int acc = g.K % 16 ? (int)ACC_F16 : g.acc;
     const TileTimes t = tile_times(acc, 2.0 * (double)((g.K + 2 * TILE_K - 1) / (2 * TILE_K)));
-    const int64_t tiles_m = (g.M + TILE_M - 1) / TILE_M;
-    auto rounds = [&](int64_t width) { return (double)((tiles_m * ((p.N + width - 1) / width) + 255) / 256); };
-    const int forced = knob(FP8_KNOB_TILE_N);
-    return {false, true, SMALL_NONE, acc, forced ? forced : rounds(128) * t.narrow < rounds(256) * t.wide ? 128 : 256};
+    const double own = o.op == OP_GATED_GRAD ? 25.0 : o.op == OP_GATED ? 3.0 : o.op == OP_ACT_GRAD || o.side ? 12.0 : 7.0;
+    const double wide = t.wide + own, narrow = t.narrow + 0.5 * own;
+    const int64_t tiles_m = (g.M + TILE_M - 1) / TILE_M, wide_all = (p.N + 255) / 256, narrow_all = (p.N + 127) / 128;
+    const double us_wide = tiles_makespan(tiles_m * wide_all, 0, wide, narrow), us_narrow = tiles_makespan(0, tiles_m * narrow_all, wide, narrow);
+    OpPlan r = {false, true, SMALL_NONE, acc, us_narrow < us_wide ? 128 : 256, 0};
+    const int forced = knob(FP8_KNOB_TILE_N), mixed = knob(FP8_KNOB_MIXED);
+    if (forced) r.tile_n = forced;
+    if (forced || mixed == 1 || wide_all < 2 || (mixed == 0 && tiles_m * wide_all > 16 * 256)) return r;
+    double best = 0.97 * std::min(us_wide, us_narrow);
+    if (mixed == 2) best = 1e300;
+    // (as many wide columns as whole rounds hold; fewer or more leave units idle between the widths)
+    for (int64_t units = 256; units / tiles_m < wide_all && (mixed == 2 || units <= 16 * 256); units += 256) {
+        const int64_t c = std::max<int64_t>(units / tiles_m, 1);
+        const double us = tiles_makespan(tiles_m * c, tiles_m * ((p.N - c * 256 + 127) / 128), wide, narrow) + 3.0;
+        if (c < wide_all && us < best) { best = us; r.wide_cols = (int)c; }
+    }
+    return r;
 }
 
 }  // namespace
@@ -189,7 +206,7 @@ int launch_gemm_op(const GemmArgs& g, const OpArgs& o, float* dbias)
             if (int e = launch_generic(g, o, parts)) return e;
         } else {
             GemmArgs p = g;
-            p.acc = plan.acc; p.tile_n = plan.tile_n;
+            p.acc = plan.acc; p.tile_n = plan.tile_n; p.wide_cols = plan.wide_cols;
             if (int e = plan.tiled ? tiled[order][plan.acc == ACC_FP8 ? 1 : 0](p, o) : small[order](p, o, plan.small)) return e;
             const int64_t rows = plan.tiled ? 128 : plan.small == SMALL_32x32 || plan.small == SMALL_32x64 ? 32 : 64;
             parts = (g.M + rows - 1) / rows;

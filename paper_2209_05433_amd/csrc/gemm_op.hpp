@@ -49,8 +49,8 @@ int FP8MM_OP_SMALL_NAME(2)(const GemmArgs& g, const OpArgs& o, int form);
 int FP8MM_OP_SMALL_NAME(3)(const GemmArgs& g, const OpArgs& o, int form);
 
 // The tiled kernel (gemm_op_tiled.hip), one translation unit per (storage orders, accumulation mode); g.tile_n: 256 or 128 columns of
-// op(B).  The conditions of the plain product's tiled kernel, and for the gated block a second projection that begins on a 16-byte boundary less
-// than 2^32 bytes behind the first.
+// op(B); g.wide_cols > 0: that many tile columns of 256 and narrow ones for the rest.  The conditions of the plain product's tiled kernel; B in E4M3 (as weights and activations are); for the gated block a second projection
+// that begins on a 16-byte boundary less than 2^32 bytes behind the first.
 #define FP8MM_OP_TILED_NAME_(l, a) launch_op_tiled_l##l##_a##a
 #define FP8MM_OP_TILED_NAME(l, a) FP8MM_OP_TILED_NAME_(l, a)
 #define FP8MM_DECLARE_OP_TILED(l) \
@@ -74,10 +74,12 @@ typedef float op_f32x2 __attribute__((ext_vector_type(2)));
 
 // ---- activations ------------------------------------------------------------------------------------------------
 // With s(t) = 1 / (1 + e^-t): SiLU z s(z); GELU z Phi(z); its tanh form z s(2 k (z + 0.044715 z^3)), k = sqrt(2 / pi), since
-// (1 + tanh t) / 2 = s(2 t).  Beyond |z| = 16 the tails are 0 and 1 in 32 bits; the polynomial and the products of the derivative are
-// taken of the clamped z (NaN passes), so that nothing there becomes inf x 0.  act(-inf) is the limit, 0; NaN stays NaN.
-// The exponential and the reciprocal are the instructions (1 ulp each).
-__device__ __forceinline__ float op_clamp(float z, float most) { return z > most ? most : z < -most ? -most : z; }
+// (1 + tanh t) / 2 = s(2 t).  The exponential and the reciprocal are the instructions (1 ulp each).  Phi by Hastings' rational
+// approximation of the error function (Abramowitz and Stegun 7.1.26): with x = |z| / sqrt(2) and t = 1 / (1 + 0.3275911 x) it is
+// 1 - Phi(|z|) = t (a1 + t (a2 + ...)) e^(-x^2) / 2 within 7.5e-8, 20 instruction slots with the derivative's density in them for free (the
+// library's erff: about 100, and 4096 x 6144 outputs spent 15 us a round in it).
+// Beyond |z| = 16 (SiLU: 128) the tails are 0 and 1 in 32 bits; where z would come in as inf x 0 it is held there (a NaN comes through the other
+// factor): act(-inf) is the limit, 0.
 __device__ __forceinline__ float op_sigmoid(float t) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * t)); }
 
 template <int ACT>
@@ -89,37 +91,43 @@ __device__ __forceinline__ void act_both(float z, float& value, float& slope)
         value = z < 0.0f ? 0.0f : z;
         slope = z > 0.0f ? 1.0f : z <= 0.0f ? 0.0f : z;
     } else if (ACT == FP8_ACT_SILU) {
-        const float zc = op_clamp(z, 128.0f), s = op_sigmoid(zc);
-        value = (z < -128.0f ? -128.0f : z) * s;
-        slope = s * (1.0f + zc * (1.0f - s));
+        const float s = op_sigmoid(z);
+        value = __builtin_amdgcn_fmed3f(z, -128.0f, __builtin_inff()) * s;
+        slope = s * __builtin_fmaf(__builtin_amdgcn_fmed3f(z, -128.0f, 128.0f), 1.0f - s, 1.0f);
     } else if (ACT == FP8_ACT_GELU) {
-        const float zc = op_clamp(z, 16.0f), p = 0.5f + 0.5f * erff(0.70710678f * zc);
-        value = (z < -16.0f ? -16.0f : z) * p;
-        slope = p + zc * (0.39894228f * __builtin_amdgcn_exp2f(-0.72134752f * zc * zc));
+        const float e = __builtin_amdgcn_exp2f(-0.72134752f * z * z);                         // e^(-z^2 / 2)
+        const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.23164191f, __builtin_fabsf(z), 1.0f));
+        float q = __builtin_fmaf(0.530702714f, t, -0.726576013f);                               // (the halves of a5 .. a1)
+        q = __builtin_fmaf(q, t, 0.710706870f);
+        q = __builtin_fmaf(q, t, -0.142248368f);
+        q = __builtin_fmaf(q, t, 0.127414796f) * t * e;
+        const float p = z < 0.0f ? q : 1.0f - q;
+        value = __builtin_amdgcn_fmed3f(z, -16.0f, __builtin_inff()) * p;
+        slope = __builtin_fmaf(__builtin_amdgcn_fmed3f(z, -16.0f, 16.0f) * 0.39894228f, e, p);
     } else {
-        const float zc = op_clamp(z, 16.0f), q = zc * zc;
-        const float s = op_sigmoid(1.59576912f * zc * (1.0f + 0.044715f * q));
-        value = (z < -16.0f ? -16.0f : z) * s;
-        slope = s + zc * s * (1.0f - s) * 1.59576912f * (1.0f + 0.134145f * q);
+        const float zc = __builtin_amdgcn_fmed3f(z, -16.0f, 16.0f), q = z == z ? zc * zc : z;
+        const float s = op_sigmoid(1.59576912f * zc * __builtin_fmaf(0.044715f, q, 1.0f));
+        value = __builtin_amdgcn_fmed3f(z, -16.0f, __builtin_inff()) * s;
+        slope = __builtin_fmaf(zc * s * (1.0f - s) * 1.59576912f, __builtin_fmaf(0.134145f, q, 1.0f), s);
     }
 }
 
-template <int W, int ACT>
-__device__ __forceinline__ void act_each(const float (&z)[W], float (&value)[W], float (&slope)[W])
+template <int E, int ACT>
+__device__ __forceinline__ void act_each(const float (&z)[E], float (&value)[E], float (&slope)[E])
 {
 #pragma unroll
-    for (int i = 0; i < W; ++i) act_both<ACT>(z[i], value[i], slope[i]);
+    for (int i = 0; i < E; ++i) act_both<ACT>(z[i], value[i], slope[i]);
 }
 
-template <int W>
-__device__ __forceinline__ void act_row(int act, const float (&z)[W], float (&value)[W], float (&slope)[W])
+template <int E>
+__device__ __forceinline__ void act_all(int act, const float (&z)[E], float (&value)[E], float (&slope)[E])
 {
     switch (act) {
-        case FP8_ACT_NONE: act_each<W, FP8_ACT_NONE>(z, value, slope); break;
-        case FP8_ACT_RELU: act_each<W, FP8_ACT_RELU>(z, value, slope); break;
-        case FP8_ACT_GELU: act_each<W, FP8_ACT_GELU>(z, value, slope); break;
-        case FP8_ACT_SILU: act_each<W, FP8_ACT_SILU>(z, value, slope); break;
-        default: act_each<W, FP8_ACT_GELU_TANH>(z, value, slope); break;
+        case FP8_ACT_NONE: act_each<E, FP8_ACT_NONE>(z, value, slope); break;
+        case FP8_ACT_RELU: act_each<E, FP8_ACT_RELU>(z, value, slope); break;
+        case FP8_ACT_GELU: act_each<E, FP8_ACT_GELU>(z, value, slope); break;
+        case FP8_ACT_SILU: act_each<E, FP8_ACT_SILU>(z, value, slope); break;
+        default: act_each<E, FP8_ACT_GELU_TANH>(z, value, slope); break;
     }
 }
 
@@ -163,113 +171,188 @@ __device__ __forceinline__ void load_row(const void* p, int dtype, int64_t at, i
     }
 }
 
-// out_kind: as of the product's output (the first two are fp8_dtype_t); sD: of FP8 kinds.  quad_max: the largest magnitude of v as bits.
-template <int W>
-__device__ __forceinline__ void store_row(void* p, int out_kind, int64_t at, int left, const float (&v)[W], float sD, unsigned max_bits)
+// Where G rows of W values go: the index of each row's first value, how many of the W columns are inside, which of the rows (whole: all rows
+// and columns, the same for the wave).
+template <int G> struct RowsAt { int64_t at[G]; int left; unsigned rows; bool whole; };
+
+template <int G, int W, class F>
+__device__ __forceinline__ void each_row(const RowsAt<G>& t, F store)
 {
-    if (out_kind == OUT_F32) {
-        float* f = (float*)p + at;
-        if (left >= W) {
+    if (t.whole) {
 #pragma unroll
-            for (int i = 0; i < W / 4; ++i)
-                *(u32x4_any*)(f + 4 * i) = (u32x4){as_u32(v[4 * i]), as_u32(v[4 * i + 1]), as_u32(v[4 * i + 2]), as_u32(v[4 * i + 3])};
-        } else {
+        for (int g = 0; g < G; ++g) store(g);
+    } else {
 #pragma unroll
-            for (int i = 0; i < W - 1; ++i) if (i < left) f[i] = v[i];
-        }
-    } else if (out_kind == OUT_BF16) {
-        unsigned short* h = (unsigned short*)p + at;
-        unsigned x[W / 2];
+        for (int g = 0; g < G; ++g) if (t.rows >> g & 1) store(g);
+    }
+}
+
+// out_kind: as of a product's output (the first two are fp8_dtype_t); sD: of FP8 kinds, max_bits: the largest magnitude of v there, as bits.
+template <int G, int W>
+__device__ __forceinline__ void store_rows(void* p, int out_kind, const RowsAt<G>& t, const float (&v)[G * W], float sD, unsigned max_bits)
+{
+    if (out_kind == OUT_BF16) {
+        unsigned x[G * W / 2];
 #pragma unroll
-        for (int j = 0; j < W / 2; ++j) x[j] = __builtin_bit_cast(unsigned, __builtin_convertvector((op_f32x2){v[2 * j], v[2 * j + 1]}, op_bf16x2));
-        if (left >= W) {
-            if (W == 8) *(u32x4_any*)h = (u32x4){x[0], x[1], x[W / 2 - 2], x[W / 2 - 1]};
-            else *(u32x2_any*)h = (u32x2){x[0], x[1]};
-        } else {
+        for (int j = 0; j < G * W / 2; ++j) x[j] = __builtin_bit_cast(unsigned, __builtin_convertvector((op_f32x2){v[2 * j], v[2 * j + 1]}, op_bf16x2));
+        each_row<G, W>(t, [&](int g) __attribute__((always_inline)) {
+            unsigned short* h = (unsigned short*)p + t.at[g];
+            const unsigned* r = x + g * (W / 2);
+            if (t.whole || t.left >= W) {
+                if (W == 8) *(u32x4_any*)h = (u32x4){r[0], r[1], r[W / 2 - 2], r[W / 2 - 1]};
+                else *(u32x2_any*)h = (u32x2){r[0], r[1]};
+            } else {
 #pragma unroll
-            for (int i = 0; i < W - 1; ++i) if (i < left) h[i] = (unsigned short)(x[i >> 1] >> (16 * (i & 1)));
-        }
+                for (int i = 0; i < W - 1; ++i) if (i < t.left) h[i] = (unsigned short)(r[i >> 1] >> (16 * (i & 1)));
+            }
+        });
+    } else if (out_kind == OUT_F32) {
+        each_row<G, W>(t, [&](int g) __attribute__((always_inline)) {
+            float* f = (float*)p + t.at[g];
+            const float* r = v + g * W;
+            if (t.whole || t.left >= W) {
+#pragma unroll
+                for (int i = 0; i < W / 4; ++i)
+                    *(u32x4_any*)(f + 4 * i) = (u32x4){as_u32(r[4 * i]), as_u32(r[4 * i + 1]), as_u32(r[4 * i + 2]), as_u32(r[4 * i + 3])};
+            } else {
+#pragma unroll
+                for (int i = 0; i < W - 1; ++i) if (i < t.left) f[i] = r[i];
+            }
+        });
     } else {
         // (the largest product tells whether anything has to be clamped or looked at one by one)
         const bool e4m3 = out_kind == OUT_E4M3, inside = __builtin_fabsf(as_f32(max_bits) * sD) <= (e4m3 ? 448.0f : 57344.0f);
-        unsigned x[W / 4];
+        unsigned x[G * W / 4];
+        float y[G * W];
 #pragma unroll
-        for (int j = 0; j < W / 4; ++j) {
-            const float a = v[4 * j] * sD, b = v[4 * j + 1] * sD, c = v[4 * j + 2] * sD, d = v[4 * j + 3] * sD;
-            x[j] = inside ? (e4m3 ? encode4_inside<FP8_E4M3>(a, b, c, d) : encode4_inside<FP8_E5M2>(a, b, c, d))
-                          : (e4m3 ? encode4<FP8_E4M3>(a, b, c, d) : encode4<FP8_E5M2>(a, b, c, d));
-        }
-        uint8_t* q = (uint8_t*)p + at;
-        if (left >= W) {
-            if (W == 8) *(u32x2_any*)q = (u32x2){x[0], x[W / 4 - 1]};
-            else *(unsigned __attribute__((aligned(1)))*)q = x[0];
+        for (int j = 0; j < G * W; ++j) y[j] = v[j] * sD;
+        if (__all(inside)) {
+            if (e4m3) {
+#pragma unroll
+                for (int j = 0; j < G * W / 4; ++j) x[j] = encode4_inside<FP8_E4M3>(y[4 * j], y[4 * j + 1], y[4 * j + 2], y[4 * j + 3]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < G * W / 4; ++j) x[j] = encode4_inside<FP8_E5M2>(y[4 * j], y[4 * j + 1], y[4 * j + 2], y[4 * j + 3]);
+            }
         } else {
 #pragma unroll
-            for (int i = 0; i < W - 1; ++i) if (i < left) q[i] = (uint8_t)(x[i >> 2] >> (8 * (i & 3)));
+            for (int j = 0; j < G * W / 4; ++j)
+                x[j] = e4m3 ? encode4<FP8_E4M3>(y[4 * j], y[4 * j + 1], y[4 * j + 2], y[4 * j + 3]) : encode4<FP8_E5M2>(y[4 * j], y[4 * j + 1], y[4 * j + 2], y[4 * j + 3]);
         }
-    }
-}
-
-// NaN patterns sort above infinity.
-template <int W>
-__device__ __forceinline__ unsigned max_bits_of(const float (&v)[W], int left)
-{
-    unsigned m = 0;
+        each_row<G, W>(t, [&](int g) __attribute__((always_inline)) {
+            uint8_t* q = (uint8_t*)p + t.at[g];
+            const unsigned* r = x + g * (W / 4);
+            if (t.whole || t.left >= W) {
+                if (W == 8) *(u32x2_any*)q = (u32x2){r[0], r[W / 4 - 1]};
+                else *(unsigned __attribute__((aligned(1)))*)q = r[0];
+            } else {
 #pragma unroll
-    for (int i = 0; i < W; ++i) m = max(m, i < left ? as_u32(v[i]) & 0x7fffffffu : 0u);
-    return m;
+                for (int i = 0; i < W - 1; ++i) if (i < t.left) q[i] = (uint8_t)(r[i >> 2] >> (8 * (i & 3)));
+            }
+        });
+    }
 }
 
 // ---- sums -> outputs ---------------------------------------------------------------------------------------------------
-// W columns from `col` on of row `row`, `left` (>= 1) of them inside; y, u: the values of c (u: of the second projection).  y is left as
-// what goes into the column sums (zeros outside).  Returns the largest |output| as bits.
+// Which G rows of an output a lane finishes: W columns from `col` on, `left` of them inside (>= 1 for a lane with rows).
+template <int G> struct OutRows { int64_t row[G]; int64_t col; int left; unsigned rows; bool whole; };
+
+template <int G>
+__device__ __forceinline__ RowsAt<G> rows_at(const OutRows<G>& t, int64_t width, int64_t more)
+{
+    RowsAt<G> r;
+#pragma unroll
+    for (int g = 0; g < G; ++g) r.at[g] = t.row[g] * width + t.col + more;
+    r.left = t.left; r.rows = t.rows; r.whole = t.whole;
+    return r;
+}
+
+// Zeros in the place of what lies outside.
+template <int G, int W>
+__device__ __forceinline__ void zero_outside(const OutRows<G>& t, float (&v)[G * W])
+{
+    if (t.whole) return;
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int i = 0; i < W; ++i) v[g * W + i] = (t.rows >> g & 1) && i < t.left ? v[g * W + i] : 0.0f;
+}
+
+// The largest magnitude as bits (a NaN stays one: its pattern sorts above infinity).
+template <int E>
+__device__ __forceinline__ unsigned max_bits_of(const float (&v)[E])
+{
+    float m = 0.0f;
+#pragma unroll
+    for (int i = 0; i < E; ++i) m = __builtin_elementwise_maximum(m, __builtin_fabsf(v[i]));     // (two values an instruction)
+    return as_u32(m) & 0x7fffffffu;
+}
+
+// y, u: the values of c (u: of the second projection); a, b: what o.side has there (b: of the second projection; OP_ACT: a is zero
+// without a residual).  OP_ACT_GRAD leaves in y what goes into the column sums (zeros outside).  Returns the largest |output| as bits, where
+// somebody wants it.  Several rows at a time, so that the branches on the call's kinds are taken once for all of them: with one wave a SIMD
+// nothing hides a branch either (8 values a time: 945 cycles of a 256-wide tile's end were 60 instructions and 15 branches).
+template <int G, int W, int OP>
+__device__ __forceinline__ unsigned op_finish(const OpArgs& o, void* D, int64_t N, const OutRows<G>& t, float (&y)[G * W], float (&u)[G * W], const float (&bias)[W],
+                                              const float (&a)[G * W], const float (&b)[G * W], float sD)
+{
+    constexpr int E = G * W;
+    const bool want_top = o.amax_out != nullptr || o.out_kind >= OUT_E4M3;
+    float value[E], slope[E];
+    unsigned top = 0;
+    if (OP == OP_ACT || OP == OP_GATED) {
+        if (OP == OP_ACT) {
+#pragma unroll
+            for (int i = 0; i < E; ++i) y[i] += bias[i % W];
+        }
+        if (o.kept) {
+            store_rows<G, W>(o.kept, o.kept_dtype, rows_at(t, OP == OP_GATED ? 2 * N : N, 0), y, 1.0f, 0);
+            if (OP == OP_GATED) store_rows<G, W>(o.kept, o.kept_dtype, rows_at(t, 2 * N, N), u, 1.0f, 0);
+        }
+        act_all<E>(o.act, y, value, slope);
+#pragma unroll
+        for (int i = 0; i < E; ++i) value[i] = OP == OP_GATED ? value[i] * u[i] : value[i] + a[i];
+        if (want_top) {
+            zero_outside<G, W>(t, value);
+            top = max_bits_of<E>(value);
+        }
+        store_rows<G, W>(D, o.out_kind, rows_at(t, N, 0), value, sD, top);
+        return top;
+    }
+    act_all<E>(o.act, a, value, slope);
+    const int64_t width = OP == OP_GATED_GRAD ? 2 * N : N;
+    unsigned top_u = 0;
+    if (OP == OP_GATED_GRAD) {
+#pragma unroll
+        for (int i = 0; i < E; ++i) { value[i] *= y[i]; slope[i] *= b[i]; }
+        if (want_top) {
+            zero_outside<G, W>(t, value);
+            top_u = max_bits_of<E>(value);
+        }
+        store_rows<G, W>(D, o.out_kind, rows_at(t, width, N), value, sD, top_u);
+    }
+#pragma unroll
+    for (int i = 0; i < E; ++i) y[i] *= slope[i];
+    if (want_top || o.sums) zero_outside<G, W>(t, y);
+    if (want_top) top = max_bits_of<E>(y);
+    store_rows<G, W>(D, o.out_kind, rows_at(t, width, 0), y, sD, top);
+    return max(top, top_u);
+}
+
+// One row of W columns, `left` (>= 1) of them inside, with o.side read here.  PAIR: OP_GATED, else one of the others.
 template <int W, bool PAIR>
-__device__ __forceinline__ unsigned op_row(const OpArgs& o, void* D, int64_t N, int64_t row, int64_t col, int left, float (&y)[W], const float (&u)[W],
+__device__ __forceinline__ unsigned op_row(const OpArgs& o, void* D, int64_t N, int64_t row, int64_t col, int left, float (&y)[W], float (&u)[W],
                                            const float (&bias)[W], float sD)
 {
-    float value[W], slope[W], side[W];
-    if (PAIR) {                                                           // OP_GATED
-        if (o.kept) {
-            store_row<W>(o.kept, o.kept_dtype, row * 2 * N + col, left, y, 1.0f, 0);
-            store_row<W>(o.kept, o.kept_dtype, row * 2 * N + N + col, left, u, 1.0f, 0);
-        }
-        act_row<W>(o.act, y, value, slope);
-#pragma unroll
-        for (int i = 0; i < W; ++i) value[i] *= u[i];
-        const unsigned top = max_bits_of<W>(value, left);
-        store_row<W>(D, o.out_kind, row * N + col, left, value, sD, top);
-        return top;
-    }
-    if (o.op == OP_ACT) {
-#pragma unroll
-        for (int i = 0; i < W; ++i) y[i] += bias[i];
-        if (o.kept) store_row<W>(o.kept, o.kept_dtype, row * N + col, left, y, 1.0f, 0);
-        act_row<W>(o.act, y, value, slope);
-        if (o.side) {
-            load_row<W>(o.side, o.side_dtype, row * N + col, left, side);
-#pragma unroll
-            for (int i = 0; i < W; ++i) value[i] += side[i];
-        }
-        const unsigned top = max_bits_of<W>(value, left);
-        store_row<W>(D, o.out_kind, row * N + col, left, value, sD, top);
-        return top;
-    }
+    float a[W] = {}, b[W] = {};
+    const OutRows<1> t = {{row}, col, left, 1u, false};
+    if (PAIR) return op_finish<1, W, OP_GATED>(o, D, N, t, y, u, bias, a, b, sD);
     const int64_t width = o.op == OP_GATED_GRAD ? 2 * N : N;
-    load_row<W>(o.side, o.side_dtype, row * width + col, left, side);
-    act_row<W>(o.act, side, value, slope);
-    unsigned top = 0;
-    if (o.op == OP_GATED_GRAD) {
-        load_row<W>(o.side, o.side_dtype, row * width + N + col, left, side);
-#pragma unroll
-        for (int i = 0; i < W; ++i) { value[i] *= y[i]; slope[i] *= side[i]; }
-        top = max_bits_of<W>(value, left);
-        store_row<W>(D, o.out_kind, row * width + N + col, left, value, sD, top);
-    }
-#pragma unroll
-    for (int i = 0; i < W; ++i) y[i] = i < left ? y[i] * slope[i] : 0.0f;
-    const unsigned top_y = max_bits_of<W>(y, left);
-    store_row<W>(D, o.out_kind, row * width + col, left, y, sD, top_y);
-    return max(top, top_y);
+    if (o.side) load_row<W>(o.side, o.side_dtype, row * width + col, left, a);
+    if (o.op == OP_ACT) return op_finish<1, W, OP_ACT>(o, D, N, t, y, u, bias, a, b, sD);
+    if (o.op == OP_ACT_GRAD) return op_finish<1, W, OP_ACT_GRAD>(o, D, N, t, y, u, bias, a, b, sD);
+    load_row<W>(o.side, o.side_dtype, row * width + N + col, left, b);
+    return op_finish<1, W, OP_GATED_GRAD>(o, D, N, t, y, u, bias, a, b, sD);
 }
 
 // 1 / the factor of a column of the product (up: of the second projection), in 64 bits: with 1 / sA it is rounded once.

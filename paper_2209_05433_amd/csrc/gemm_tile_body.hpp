@@ -212,8 +212,8 @@ __device__ __forceinline__ void direct_load_or_zero(const uint8_t* base, unsigne
 // the dispatcher): no edge tiles, K a multiple of 128 and at least 512, per-tensor factors, fp32 or
 // bf16 output with rows on 16-byte boundaries, no output maximum, no K slices.
 //
-// OP: 0 the plain product; 1 an operator behind it, 2 the gated block, whose tile has BN / 2 output columns (both: ep is an
-// OpArgs, N counts output columns; no slices of K, not persistent).
+// OP: 0 the plain product; 1 bias, activation and residual behind it, 2 the gated block, whose tile has BN / 2 output columns, 3 the gradients
+// (1 to 3: ep is an OpArgs, N counts output columns; no slices of K, not persistent).
 //
 // The body works on tile number `bid_in` of a region of the output that starts at column n_begin and
 // is tiles_n tiles wide (the whole output for the plain kernel; see gemm_mixed_kernel).
@@ -638,6 +638,7 @@ __device__ __forceinline__ void gemm_tile_body(
     const std::integral_constant<bool, true> yes;
     const std::integral_constant<bool, false> no;
 
+    [[maybe_unused]] OpTouch<NB, OP> beside = {};
     // One round of the outer loop per tile (a single one unless PERSIST).  The tile end sits between
     // the inner loops, not inside them: inside, the accumulators would have to change register
     // class (the stores read them as vector registers, the matrix instructions keep them in the
@@ -653,6 +654,7 @@ __device__ __forceinline__ void gemm_tile_body(
             k_step(full, kt + 1, true, sa, sb, sa_n, sb_n, af1, bf1, af0, bf0, no);
             sa = sa_n; sb = sb_n;
         }
+        if constexpr (OP == 1 || OP == 3) beside.touch(static_cast<const OpArgs&>(ep), M, N, m0, n0, tid);
         for (; kt < tile_stop; kt += 2) {
             const int sa_n = A_KC ? (sa == A_RING - 1 ? 0 : sa + 1) : 0;
             const int sb_n = B_KC ? (sb == B_RING - 1 ? 0 : sb + 1) : 0;
@@ -696,7 +698,8 @@ __device__ __forceinline__ void gemm_tile_body(
 
     __builtin_amdgcn_s_waitcnt(0xC07F);
     __builtin_amdgcn_s_barrier();                           // every wave is done with the operand slabs
-    if constexpr (OP != 0) op_store_tile<NB, OP == 2>(acc, smem, static_cast<const OpArgs&>(ep), C, M, N, m0, n0, w);
+    if constexpr (OP == 1 || OP == 3) beside.touched();
+    if constexpr (OP != 0) op_store_tile<NB, OP>(acc, smem, static_cast<const OpArgs&>(ep), C, M, N, m0, n0, w);
     else store_tile<NB, false>(acc, smem, ep, C, M, N, m0, n0, w);
 }
 
