@@ -31,7 +31,7 @@ UNITS = [("gemm_tiled.hip", ["-DFP8MM_LAYOUT=%d" % k, "-DFP8MM_ACC=%d" % a], "ge
         [("gemm_dispatch.hip", [], "gemm_dispatch.o"), ("gemm_splitk.hip", [], "gemm_splitk.o"),
          ("cast_kernels.hip", [], "cast_kernels.o"),
          ("cast_variants.hip", [], "cast_variants.o"),
-         ("gemm_op.hip", [], "gemm_op.o"), ("grad_clip.hip", [], "grad_clip.o"), ("api_op.hip", [], "api_op.o"),
+         ("gemm_op.hip", [], "gemm_op.o"), ("gemm_op_skinny.hip", [], "gemm_op_skinny.o"), ("grad_clip.hip", [], "grad_clip.o"), ("api_op.hip", [], "api_op.o"),
          ("api.hip", [], "api.o")]
 
 # -packed-fp32-ops is switched off on purpose: the compiler must not form packed fp32

@@ -91,7 +91,14 @@ __global__ __launch_bounds__(256) void gemm_op_generic_kernel(const uint8_t* __r
             o.sums[tm * N + n0 + tid] = s;
         }
     }
-    if (o.amax_out) wave_amax_commit(top, o.amax_out);
+    if (o.amax_out) {
+        __shared__ unsigned tops[4];
+#pragma unroll
+        for (int d = 32; d >= 1; d >>= 1) top = max(top, (unsigned)__shfl_xor((int)top, d, 64));
+        if ((tid & 63) == 0) tops[tid >> 6] = top;
+        __syncthreads();
+        if (tid < 64) op_commit_top(o, tid < 4 ? tops[tid] : 0u);
+    }
 }
 
 template <int FA, int FB>
@@ -101,11 +108,10 @@ void enqueue_generic(const GemmArgs& g, const OpArgs& o, unsigned tiles)
     else enqueue(gemm_op_generic_kernel<FA, FB, false>, dim3(tiles), dim3(256), 0, g.stream, g.A, g.B, g.C, g.M, g.N, g.K, o, g.transA, g.transB);
 }
 
-int launch_generic(const GemmArgs& g, const OpArgs& o, int64_t& parts)
+int launch_generic(const GemmArgs& g, const OpArgs& o)
 {
     const int64_t tiles = ((g.M + GT - 1) / GT) * ((g.N + GT - 1) / GT);
     if (tiles > 0x7fffffffll) return fail(FP8_ERR_UNSUPPORTED, "gemm with an operator: %lld tiles of 64 x 64 exceed the grid limit", (long long)tiles);
-    parts = (g.M + GT - 1) / GT;
     if (g.fmtA == FP8_E4M3) {
         if (g.fmtB == FP8_E4M3) enqueue_generic<FP8_E4M3, FP8_E4M3>(g, o, (unsigned)tiles);
         else enqueue_generic<FP8_E4M3, FP8_E5M2>(g, o, (unsigned)tiles);
@@ -119,12 +125,23 @@ int launch_generic(const GemmArgs& g, const OpArgs& o, int64_t& parts)
 __global__ void op_zero_cell_kernel(unsigned* p) { *p = 0u; }
 
 // dbias_j = sum of the rows of partial sums, always in the same order: a workgroup of 4 waves takes 64 columns, wave w the rows w, w + 4, ...
-// No rows: zeros.
-__global__ __launch_bounds__(256) void column_sum_kernel(const float* __restrict__ sums, int64_t parts, int64_t N, float* __restrict__ dbias)
+// No rows: zeros.  The workgroup behind the last columns reduces the maxima of the product's workgroups, where those are left in memory.
+__global__ __launch_bounds__(256) void column_sum_kernel(const float* __restrict__ sums, int64_t parts, int64_t N, float* __restrict__ dbias,
+                                                         const unsigned* __restrict__ tops, unsigned ntops, unsigned* __restrict__ amax_out)
 {
     __shared__ float part[4][64];
     const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
     const int64_t col = (int64_t)blockIdx.x * 64 + l;
+    if (tops && blockIdx.x == gridDim.x - 1) {
+        unsigned m = 0;
+        for (unsigned i = threadIdx.x; i < ntops; i += 256) m = max(m, tops[i]);
+#pragma unroll
+        for (int d = 32; d >= 1; d >>= 1) m = max(m, (unsigned)__shfl_xor((int)m, d, 64));
+        if (l == 0) part[w][0] = as_f32(m);
+        __syncthreads();
+        if (threadIdx.x == 0) *amax_out = max(max(as_u32(part[0][0]), as_u32(part[1][0])), max(as_u32(part[2][0]), as_u32(part[3][0])));
+        return;
+    }
     float s = 0.0f;
     if (col < N)
         for (int64_t i = w; i < parts; i += 4) s += sums[i * N + col];
@@ -134,21 +151,23 @@ __global__ __launch_bounds__(256) void column_sum_kernel(const float* __restrict
 }
 
 // Which kernel takes the call, as for the plain product of the same operands.
-struct OpPlan { bool generic, tiled; int small, acc, tile_n, wide_cols; };
+struct OpPlan { bool generic, tiled; int small, acc, tile_n, wide_cols; bool skinny; };
 OpPlan plan_op(const GemmArgs& g, const OpArgs& o)
 {
     const bool pair = op_pair_in(o.op);
-    const OpPlan plain_fmas = {true, false, SMALL_NONE, 0, 0, 0};
+    const OpPlan plain_fmas = {true, false, SMALL_NONE, 0, 0, 0, false};
     GemmArgs p = g;
     if (pair) p.N = 2 * g.N;
     p.ep = o;
     p.ep.b_per_col = o.b_factors != B_ONE;
     if (g.K == 0 || (pair && !g.transB && g.N < 16)) return plain_fmas;
+    const bool chosen = !knob(FP8_KNOB_SMALL) && !knob(FP8_KNOB_GEMM_KERNEL) && !knob(FP8_KNOB_TILE_N);      // no knob asks for another kernel
+    if (chosen && op_skinny_takes(g, pair)) return {false, false, SMALL_NONE, (int)ACC_F16, 0, 0, true};
     const GemmPlan plan = plan_gemm(p, false);
     if (plan.kernel == GEMM_GENERIC) return plain_fmas;
-    if (plan.small != SMALL_NONE) return {false, false, plan.small, g.acc, 0, 0};
+    if (plan.small != SMALL_NONE) return {false, false, plan.small, g.acc, 0, 0, false};
     const bool tiled = plan.kernel != GEMM_MFMA_ANY && g.fmtB == FP8_E4M3 && (!pair || (g.transB ? (uint64_t)(g.N + TILE_M) * (uint64_t)g.K < (1ull << 32) : g.N % 16 == 0));
-    if (!tiled) return ((g.M + 63) / 64) * ((p.N + 63) / 64) > 0x7fffffffll ? plain_fmas : OpPlan{false, false, SMALL_64x64, g.acc, 0, 0};
+    if (!tiled) return ((g.M + 63) / 64) * ((p.N + 63) / 64) > 0x7fffffffll ? plain_fmas : OpPlan{false, false, SMALL_64x64, g.acc, 0, 0, false};
     // The width whose rounds of 256 workgroups take less time, or both widths in one launch, by the plain product's model of run times with the
     // operator's own time on top (us of a 256-wide tile: fitted to 8192 x 8192 outputs over K = 256; it is the same per output in both widths).
     const int acc = g.K % 16 ? (int)ACC_F16 : g.acc;
@@ -157,17 +176,20 @@ OpPlan plan_op(const GemmArgs& g, const OpArgs& o)
     const double wide = t.wide + own, narrow = t.narrow + 0.5 * own;
     const int64_t tiles_m = (g.M + TILE_M - 1) / TILE_M, wide_all = (p.N + 255) / 256, narrow_all = (p.N + 127) / 128;
     const double us_wide = tiles_makespan(tiles_m * wide_all, 0, wide, narrow), us_narrow = tiles_makespan(0, tiles_m * narrow_all, wide, narrow);
-    OpPlan r = {false, true, SMALL_NONE, acc, us_narrow < us_wide ? 128 : 256, 0};
+    OpPlan r = {false, true, SMALL_NONE, acc, us_narrow < us_wide ? 128 : 256, 0, false};
     const int forced = knob(FP8_KNOB_TILE_N), mixed = knob(FP8_KNOB_MIXED);
     if (forced) r.tile_n = forced;
-    if (forced || mixed == 1 || wide_all < 2 || (mixed == 0 && tiles_m * wide_all > 16 * 256)) return r;
+    if (forced || mixed == 1 || wide_all < 2) return r;
+    if (mixed == 2) {
+        r.wide_cols = (int)(wide_all / 2);
+        return r;
+    }
+    // (as many wide columns as whole rounds hold: fewer or more leave units idle between the widths; beyond 16 rounds the last one matters little)
     double best = 0.97 * std::min(us_wide, us_narrow);
-    if (mixed == 2) best = 1e300;
-    // (as many wide columns as whole rounds hold; fewer or more leave units idle between the widths)
-    for (int64_t units = 256; units / tiles_m < wide_all && (mixed == 2 || units <= 16 * 256); units += 256) {
+    for (int64_t units = 256; units / tiles_m < wide_all && tiles_m * wide_all <= 16 * 256; units += 256) {
         const int64_t c = std::max<int64_t>(units / tiles_m, 1);
         const double us = tiles_makespan(tiles_m * c, tiles_m * ((p.N - c * 256 + 127) / 128), wide, narrow) + 3.0;
-        if (c < wide_all && us < best) { best = us; r.wide_cols = (int)c; }
+        if (us < best) { best = us; r.wide_cols = (int)c; }
     }
     return r;
 }
@@ -186,34 +208,47 @@ int raise_lds_limit(const void* kernel, int bytes, std::atomic<unsigned long lon
     return FP8_OK;
 }
 
-int launch_gemm_op(const GemmArgs& g, const OpArgs& o, float* dbias)
+int launch_gemm_op(const GemmArgs& g, const OpArgs& args, float* dbias)
 {
-    if (dbias && g.N > (int64_t)0x7fffffff * 64) return fail(FP8_ERR_UNSUPPORTED, "gemm with an operator: dbias of %lld values exceeds the grid limit", (long long)g.N);
-    if (o.amax_out) {                                        // written, not accumulated
+    typedef int (*small_fn)(const GemmArgs&, const OpArgs&, int);
+    static const small_fn small[4] = {FP8MM_OP_SMALL_NAME(0), FP8MM_OP_SMALL_NAME(1), FP8MM_OP_SMALL_NAME(2), FP8MM_OP_SMALL_NAME(3)};
+    typedef int (*tiled_fn)(const GemmArgs&, const OpArgs&);
+    static const tiled_fn tiled[4][2] = {{FP8MM_OP_TILED_NAME(0, 0), FP8MM_OP_TILED_NAME(0, 1)}, {FP8MM_OP_TILED_NAME(1, 0), FP8MM_OP_TILED_NAME(1, 1)},
+                                         {FP8MM_OP_TILED_NAME(2, 0), FP8MM_OP_TILED_NAME(2, 1)}, {FP8MM_OP_TILED_NAME(3, 0), FP8MM_OP_TILED_NAME(3, 1)}};
+    if (dbias && g.N > (int64_t)0x7fffffff * 32) return fail(FP8_ERR_UNSUPPORTED, "gemm with an operator: dbias of %lld values exceeds the grid limit", (long long)g.N);
+    const bool work = g.M > 0 && g.N > 0;
+    OpArgs o = args;
+    OpPlan plan{};
+    int64_t parts = 0, tops = 0;                             // rows of partial sums; workgroups that leave their maxima in memory
+    if (work) {
+        plan = plan_op(g, o);
+        int64_t rows = 64, width = 64;                       // of a workgroup's outputs
+        if (plan.skinny) { rows = 16; width = 16; }
+        else if (plan.tiled) { rows = TILE_M; width = plan.tile_n; }
+        else if (plan.small == SMALL_32x32 || plan.small == SMALL_32x64) { rows = 32; width = plan.small == SMALL_32x32 ? 32 : 64; }
+        auto count = [](int64_t n, int64_t per) { return (n + per - 1) / per; };
+        parts = count(g.M, plan.tiled ? rows / 2 : rows);
+        // With a bias gradient there is a launch behind the product anyway: it takes the maxima along, if the workspace has room for them behind the
+        // partial sums (4.5 us less than a cell that has to be cleared first).
+        if (o.sums && o.amax_out) {
+            tops = count(g.M, rows) * (plan.wide_cols ? plan.wide_cols + count(g.N - plan.wide_cols * (int64_t)256, 128) : count(g.N, width));
+            if ((count(g.M, kOpSumRows) - parts) * g.N >= tops && tops <= 0x7fffffff) o.tops = (unsigned*)(o.sums + parts * g.N);
+        }
+    }
+    if (o.amax_out && !o.tops) {                             // written, not accumulated
         enqueue(op_zero_cell_kernel, dim3(1), dim3(1), 0, g.stream, (unsigned*)o.amax_out);
         if (int e = check_launch("gemm with an operator (amax init)")) return e;
     }
-    int64_t parts = 0;
-    if (g.M > 0 && g.N > 0) {
-        typedef int (*small_fn)(const GemmArgs&, const OpArgs&, int);
-        static const small_fn small[4] = {FP8MM_OP_SMALL_NAME(0), FP8MM_OP_SMALL_NAME(1), FP8MM_OP_SMALL_NAME(2), FP8MM_OP_SMALL_NAME(3)};
-        typedef int (*tiled_fn)(const GemmArgs&, const OpArgs&);
-        static const tiled_fn tiled[4][2] = {{FP8MM_OP_TILED_NAME(0, 0), FP8MM_OP_TILED_NAME(0, 1)}, {FP8MM_OP_TILED_NAME(1, 0), FP8MM_OP_TILED_NAME(1, 1)},
-                                             {FP8MM_OP_TILED_NAME(2, 0), FP8MM_OP_TILED_NAME(2, 1)}, {FP8MM_OP_TILED_NAME(3, 0), FP8MM_OP_TILED_NAME(3, 1)}};
+    if (work) {
         const int order = (g.transA ? 2 : 0) + (g.transB ? 1 : 0);
-        const OpPlan plan = plan_op(g, o);
-        if (plan.generic) {
-            if (int e = launch_generic(g, o, parts)) return e;
-        } else {
-            GemmArgs p = g;
-            p.acc = plan.acc; p.tile_n = plan.tile_n; p.wide_cols = plan.wide_cols;
-            if (int e = plan.tiled ? tiled[order][plan.acc == ACC_FP8 ? 1 : 0](p, o) : small[order](p, o, plan.small)) return e;
-            const int64_t rows = plan.tiled ? 128 : plan.small == SMALL_32x32 || plan.small == SMALL_32x64 ? 32 : 64;
-            parts = (g.M + rows - 1) / rows;
-        }
+        GemmArgs p = g;
+        p.acc = plan.acc; p.tile_n = plan.tile_n; p.wide_cols = plan.wide_cols;
+        if (int e = plan.generic ? launch_generic(g, o) : plan.skinny ? launch_op_skinny(g, o) : plan.tiled ? tiled[order][plan.acc == ACC_FP8 ? 1 : 0](p, o)
+                                                                                                            : small[order](p, o, plan.small)) return e;
     }
     if (dbias && g.N > 0) {
-        enqueue(column_sum_kernel, dim3((unsigned)((g.N + 63) / 64)), dim3(256), 0, g.stream, o.sums, parts, g.N, dbias);
+        enqueue(column_sum_kernel, dim3((unsigned)((g.N + 63) / 64) + (o.tops ? 1 : 0)), dim3(256), 0, g.stream, o.sums, parts, g.N, dbias, o.tops, (unsigned)tops,
+                (unsigned*)o.amax_out);
         return check_launch("gemm with an operator (column sums)");
     }
     return FP8_OK;

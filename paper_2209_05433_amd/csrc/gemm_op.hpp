@@ -24,6 +24,7 @@ enum { B_ONE = 0, B_PAIR = 1, B_COLUMN = 2 };
 
 struct OpArgs : EpilogueArgs {                  // (sA_dev, sB_dev: given; b_per_col: not looked at)
     float* sums;                                // null or partial column sums, a row of N for each kOpSumRows rows at least
+    unsigned* tops;                             // null or the workgroups' maxima, which then do not go to amax_out
     const void* bias;                           // null or N values
     const void* side;                           // residual (M x N or null), z (M x N), or g | u (M x 2 N)
     void* kept;                                 // null, z (M x N) or g | u (M x 2 N)
@@ -61,6 +62,10 @@ FP8MM_DECLARE_OP_TILED(1)
 FP8MM_DECLARE_OP_TILED(2)
 FP8MM_DECLARE_OP_TILED(3)
 #undef FP8MM_DECLARE_OP_TILED
+
+// The kernel of up to 16 rows (gemm_op_skinny.hip): A stored M x K, B stored N x K, rows on 16-byte boundaries, where it pays.
+bool op_skinny_takes(const GemmArgs& g, bool pair);
+int launch_op_skinny(const GemmArgs& g, const OpArgs& o);
 
 // Raises a kernel's limit of dynamic LDS, once per device (`done`: of this kernel).
 int raise_lds_limit(const void* kernel, int bytes, std::atomic<unsigned long long>& done);
@@ -353,6 +358,15 @@ __device__ __forceinline__ unsigned op_row(const OpArgs& o, void* D, int64_t N, 
     if (o.op == OP_ACT_GRAD) return op_finish<1, W, OP_ACT_GRAD>(o, D, N, t, y, u, bias, a, b, sD);
     load_row<W>(o.side, o.side_dtype, row * width + N + col, left, b);
     return op_finish<1, W, OP_GATED_GRAD>(o, D, N, t, y, u, bias, a, b, sD);
+}
+
+// The workgroup's maximum on its way out; `bits`: of the lanes of one wave.
+__device__ __forceinline__ void op_commit_top(const OpArgs& o, unsigned bits)
+{
+    if (!o.tops) { wave_amax_commit(bits, o.amax_out); return; }
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) bits = max(bits, (unsigned)__shfl_xor((int)bits, d, 64));
+    if (__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)) == 0) o.tops[blockIdx.x] = bits;
 }
 
 // 1 / the factor of a column of the product (up: of the second projection), in 64 bits: with 1 / sA it is rounded once.

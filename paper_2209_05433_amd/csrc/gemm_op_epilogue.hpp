@@ -19,8 +19,8 @@ namespace {
 // memory straight into a ring in LDS, several steps ahead, a lane's 16 bytes where the same lane reads them; waits are counted by hand.  (As loads
 // into registers the compiler waited for all of them at the first: its counts do not survive the branches around the stores.
 // 8192 x 6144 gradients of a gated block with K = 2048: 343 us unasked, 267 in registers, %% in the ring; the product alone 152.)
-constexpr int OP_RING = 71 * 1024, OP_RING_WAVE = 16 * 1024;            // LDS behind the turned rows: the waves' rings
-constexpr int OP_ROW_FACTORS = 144 * 1024, OP_COLUMN_FACTORS = 148 * 1024, OP_AMAX = 152 * 1024;        // reciprocals of factors; a word per wave
+constexpr int OP_RING = 69 * 1024, OP_RING_WAVE = 20 * 1024;            // LDS behind the turned rows: the waves' rings
+constexpr int OP_ROW_FACTORS = 149 * 1024, OP_COLUMN_FACTORS = 153 * 1024, OP_AMAX = 157 * 1024;        // reciprocals of factors; a word per wave
 
 // The vector-memory counter down to at most `allowed` (rounded down to a multiple of 4, 40 at most).
 __device__ __forceinline__ void op_wait(int allowed)
@@ -58,8 +58,8 @@ __device__ __forceinline__ void op_store_rows(v16f (&acc)[NB][4], uint8_t* smem,
     constexpr int G = BOTH ? 2 : 4;                             // rows that a lane finishes together: a step
     constexpr int STEPS = 32 * MBS / (ROWS * G), TURNS = 4 / MBS;
     constexpr int PARTS = (F32 ? 2 : 1), LOADS = G * (BOTH ? 2 : 1) * PARTS;    // requests of a step
-    constexpr int AHEAD = OP_RING_WAVE / (LOADS * 1024);        // steps that are requested ahead
-    static_assert(64 % LANES == 0 && STEPS >= 1 && (AHEAD & (AHEAD - 1)) == 0 && AHEAD >= 2 && OP_RING + 4 * OP_RING_WAVE <= OP_ROW_FACTORS, "whole rows; room for the ring");
+    constexpr int AHEAD = OP_RING_WAVE / (LOADS * 1024);        // steps (5, or 2) that are requested ahead
+    static_assert(64 % LANES == 0 && STEPS >= 1 && AHEAD >= 2 && OP_RING + 4 * OP_RING_WAVE <= OP_ROW_FACTORS, "whole rows; room for the ring");
     static_assert(4 * 32 * MBS * ROWB <= OP_RING, "room for the turned rows");
     const int l = (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));      // (see store_tile)
     const int h = l >> 5, wn = w & 1;
@@ -74,7 +74,7 @@ __device__ __forceinline__ void op_store_rows(v16f (&acc)[NB][4], uint8_t* smem,
     const unsigned ring = (unsigned)(uintptr_t)LDS_PTR(void, smem) + OP_RING + w * OP_RING_WAVE;
     const int at_col = left >= 8 ? col : N - 8;
     auto request = [&](int i) __attribute__((always_inline)) {
-        const unsigned slot = __builtin_amdgcn_readfirstlane(ring + (unsigned)(i & (AHEAD - 1)) * (LOADS * 1024));
+        const unsigned slot = __builtin_amdgcn_readfirstlane(ring + (unsigned)(i % AHEAD) * (LOADS * 1024));
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             const int64_t at = (int64_t)min(wave_m0 + (i * G + g) * ROWS + l / LANES, M - 1) * width + at_col;
@@ -169,7 +169,7 @@ __device__ __forceinline__ void op_store_rows(v16f (&acc)[NB][4], uint8_t* smem,
     const int stores = G * ((OP == OP_ACT && o.kept ? (o.kept_dtype == FP8_F32 ? 2 : 1) : 0) + (BOTH ? 2 : 1) * (o.out_kind == OUT_F32 ? 2 : 1));
     const int younger = (AHEAD - 1) * (LOADS + (inside ? stores : 0));
     auto read_beside = [&](int i, float (&a)[G * 8], float (&b)[G * 8]) __attribute__((always_inline)) {
-        const uint8_t* p = smem + OP_RING + w * OP_RING_WAVE + (i & (AHEAD - 1)) * (LOADS * 1024) + l * 16;
+        const uint8_t* p = smem + OP_RING + w * OP_RING_WAVE + (i % AHEAD) * (LOADS * 1024) + l * 16;
 #pragma unroll
         for (int g = 0; g < G; ++g)
 #pragma unroll
@@ -255,7 +255,7 @@ __device__ __forceinline__ void op_store_rows(v16f (&acc)[NB][4], uint8_t* smem,
         unsigned* cells = (unsigned*)(smem + OP_AMAX);
         if (l == 0) *LDS_PTR(unsigned, cells + w) = top;
         __syncthreads();
-        if (w == 0) wave_amax_commit(l < 4 ? *LDS_PTR(unsigned, cells + l) : 0u, o.amax_out);
+        if (w == 0) op_commit_top(o, l < 4 ? *LDS_PTR(unsigned, cells + l) : 0u);
     }
 }
 

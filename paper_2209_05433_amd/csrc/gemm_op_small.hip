@@ -274,7 +274,7 @@ __global__ __launch_bounds__(64 * NW) void gemm_op_small_kernel(const uint8_t* _
         for (int d = 32; d >= 1; d >>= 1) top = max(top, (unsigned)__shfl_xor((int)top, d, 64));
         if (l == 0) *LDS_PTR(unsigned, cells + w) = top;
         __syncthreads();
-        if (w == 0) wave_amax_commit(l < NW ? *LDS_PTR(unsigned, cells + l) : 0u, o.amax_out);
+        if (w == 0) op_commit_top(o, l < NW ? *LDS_PTR(unsigned, cells + l) : 0u);
     }
 }
 

@@ -26,7 +26,7 @@ WIDE = {F32: torch.float32, BF16: torch.bfloat16}
 # what takes a call: the library's choice, plain FMAs, tiles of the small kernel, tiles of the tiled kernel
 FORMS = {"chosen": {}, "fma": {fp8.FP8_KNOB_GEMM_KERNEL: 1}, "small_32x32": {fp8.FP8_KNOB_SMALL: 2}, "small_32x64": {fp8.FP8_KNOB_SMALL: 3},
          "small_64x64": {fp8.FP8_KNOB_SMALL: 4}, "tiled_256": {fp8.FP8_KNOB_SMALL: 1, fp8.FP8_KNOB_TILE_N: 256},
-         "tiled_128": {fp8.FP8_KNOB_SMALL: 1, fp8.FP8_KNOB_TILE_N: 128}}
+         "tiled_128": {fp8.FP8_KNOB_SMALL: 1, fp8.FP8_KNOB_TILE_N: 128}, "tiled_both": {fp8.FP8_KNOB_SMALL: 1, fp8.FP8_KNOB_MIXED: 2}}
 
 
 @contextlib.contextmanager
@@ -248,7 +248,7 @@ def run_gated_grad(c, act, kind, gu=torch.bfloat16, in_place=False, name="chosen
 
 
 # Sizes: single rows and columns, edges inside and at a tile, K below, at and beyond the chunks and stages; orders of both operands
-SIZES = [(1, 1, 1), (1, 64, 128), (3, 5, 7), (16, 48, 64), (33, 65, 100), (64, 128, 256), (100, 272, 384), (129, 320, 528), (257, 144, 1040)]
+SIZES = [(1, 1, 1), (1, 64, 128), (3, 5, 7), (16, 48, 64), (33, 65, 100), (64, 128, 256), (100, 272, 384), (129, 320, 528), (257, 144, 1040), (300, 520, 1280)]
 ORDERS = [(False, True), (False, False), (True, False), (True, True)]
 
 
@@ -413,6 +413,17 @@ def test_sums_are_the_same_in_every_run(name):
         runs.append([t.clone() for t in run_act_grad(c, "gelu", F32, name=name)])
     for r in runs[1:]:
         assert torch.equal(r[0], runs[0][0]) and torch.equal(r[1], runs[0][1])
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 2048, 6144), (1, 1000, 1008), (5, 77, 4112), (16, 4096, 2048), (13, 2000, 272), (16, 16, 16), (2, 17, 8192)])
+def test_a_few_rows(M, N, K):
+    for flags in (0, fp8.FP8_GEMM_MFMA8):
+        for fB in (E4M3, E5M2):
+            run_act(Case(M, N, K, fB=fB, flags=flags, per_row=True, factors="column", seed=1), "gelu", BF16, bias=torch.bfloat16, residual=torch.float32, z=torch.float32)
+            run_act(Case(M, N, K, fB=fB, flags=flags, seed=2), "silu", O43)
+            run_act_grad(Case(M, N, K, fA=E5M2, fB=fB, flags=flags, seed=3), "gelu_tanh", O52)
+            run_gated(Case(M, N // 2, K, wide=True, fB=fB, factors="pair", flags=flags, seed=4), "silu", O43)
+            run_gated_grad(Case(M, N, K, fA=E5M2, fB=fB, flags=flags, seed=5), "silu", F32, gu=torch.float32)
 
 
 def test_another_stream_and_graph_replays():
