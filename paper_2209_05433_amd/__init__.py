@@ -26,12 +26,12 @@ from .binding import (  # noqa: F401
 # What `import *` brings: the names above and the entry points that take tensors (looked up only where they are built).
 __all__ = [n for n in globals() if not n.startswith("_") and n != "os"]
 if os.path.exists(binding.NATIVE_PATH):
-    __all__ += binding.TENSOR_CALLS
+    __all__ += binding.TENSOR_CALLS + binding.OPERATOR_CALLS
 
 
 def __getattr__(name):
     """The entry points that take tensors: bound when first asked for, the library is loaded then."""
-    if name not in binding.TENSOR_CALLS:
+    if name not in binding.TENSOR_CALLS + binding.OPERATOR_CALLS:
         raise AttributeError("module %r has no attribute %r" % (__name__, name))
     globals()[name] = fn = getattr(binding, name)
     return fn

@@ -181,8 +181,9 @@ TENSOR_CALLS = (
     "fp8_quantize_ex", "fp8_dequantize", "fp8_quantize_amax", "fp8_quantize_sr", "fp8_scale_from_amax_history", "fp8_scale_from_amax_n",
     "fp8_amax_rows", "fp8_quantize_rows", "fp8_quantize_transpose", "fp8_gemm", "fp8_gemm_dscale", "fp8_gemm_mfma8", "fp8_gemm_mfma8_dscale",
     "fp8_gemm_ex", "fp8_gemm_splitk", "fp8_gemm_splitk_static", "fp8_gemm_fused", "fp8_scaled_gemm",
-    "fp8_gemm_act", "fp8_gemm_act_grad", "fp8_gemm_gated", "fp8_gemm_gated_grad", "fp8_grad_norm", "fp8_grad_clip",
 )
+# ... and those of the feed-forward operators.
+OPERATOR_CALLS = ("fp8_gemm_act", "fp8_gemm_act_grad", "fp8_gemm_gated", "fp8_gemm_gated_grad", "fp8_grad_norm", "fp8_grad_clip")
 
 _native = None
 
@@ -206,7 +207,7 @@ def native():
 
 def __getattr__(name):
     """Loads the binding at the first use of an entry point, not at import (the build imports this package)."""
-    if name not in TENSOR_CALLS:
+    if name not in TENSOR_CALLS + OPERATOR_CALLS:
         raise AttributeError("module %r has no attribute %r" % (__name__, name))
     globals()[name] = fn = getattr(native(), name)
     return fn

@@ -225,8 +225,10 @@ __device__ __forceinline__ void store_rows(void* p, int out_kind, const RowsAt<G
             }
         });
     } else {
-        // (the largest product tells whether anything has to be clamped or looked at one by one)
-        const bool e4m3 = out_kind == OUT_E4M3, inside = __builtin_fabsf(as_f32(max_bits) * sD) <= (e4m3 ? 448.0f : 57344.0f);
+        // (the largest product tells whether anything has to be clamped, or looked at one by one: not where all are finite.  With a factor from past maxima
+        // one of a step's thousand values lies outside the format at nearly every step)
+        const float largest = __builtin_fabsf(as_f32(max_bits) * sD);
+        const bool e4m3 = out_kind == OUT_E4M3, inside = largest <= (e4m3 ? 448.0f : 57344.0f), finite = largest < __builtin_inff();
         unsigned x[G * W / 4];
         float y[G * W];
 #pragma unroll
@@ -239,10 +241,18 @@ __device__ __forceinline__ void store_rows(void* p, int out_kind, const RowsAt<G
 #pragma unroll
                 for (int j = 0; j < G * W / 4; ++j) x[j] = encode4_inside<FP8_E5M2>(y[4 * j], y[4 * j + 1], y[4 * j + 2], y[4 * j + 3]);
             }
+        } else if (__all(finite)) {
+            if (e4m3) {
+#pragma unroll
+                for (int j = 0; j < G * W / 4; ++j) x[j] = cvt_pair<FP8_E4M3, true>(y[4 * j + 2], y[4 * j + 3], cvt_pair<FP8_E4M3, false>(y[4 * j], y[4 * j + 1], 0u));
+            } else {
+#pragma unroll
+                for (int j = 0; j < G * W / 4; ++j) x[j] = cvt_pair<FP8_E5M2, true>(y[4 * j + 2], y[4 * j + 3], cvt_pair<FP8_E5M2, false>(y[4 * j], y[4 * j + 1], 0u));
+            }
         } else {
 #pragma unroll
             for (int j = 0; j < G * W / 4; ++j)
-                x[j] = e4m3 ? encode4<FP8_E4M3>(y[4 * j], y[4 * j + 1], y[4 * j + 2], y[4 * j + 3]) : encode4<FP8_E5M2>(y[4 * j], y[4 * j + 1], y[4 * j + 2], y[4 * j + 3]);
+                x[j] = e4m3 ? encode4_bits<FP8_E4M3>(y[4 * j], y[4 * j + 1], y[4 * j + 2], y[4 * j + 3]) : encode4_bits<FP8_E5M2>(y[4 * j], y[4 * j + 1], y[4 * j + 2], y[4 * j + 3]);
         }
         each_row<G, W>(t, [&](int g) __attribute__((always_inline)) {
             uint8_t* q = (uint8_t*)p + t.at[g];
@@ -294,15 +304,14 @@ __device__ __forceinline__ unsigned max_bits_of(const float (&v)[E])
 }
 
 // y, u: the values of c (u: of the second projection); a, b: what o.side has there (b: of the second projection; OP_ACT: a is zero
-// without a residual).  OP_ACT_GRAD leaves in y what goes into the column sums (zeros outside).  Returns the largest |output| as bits, where
-// somebody wants it.  Several rows at a time, so that the branches on the call's kinds are taken once for all of them: with one wave a SIMD
+// without a residual).  OP_ACT_GRAD leaves in y what goes into the column sums (zeros outside).  Returns the largest |output| as bits.
+// Several rows at a time, so that the branches on the call's kinds are taken once for all of them: with one wave a SIMD
 // nothing hides a branch either (8 values a time: 945 cycles of a 256-wide tile's end were 60 instructions and 15 branches).
 template <int G, int W, int OP>
 __device__ __forceinline__ unsigned op_finish(const OpArgs& o, void* D, int64_t N, const OutRows<G>& t, float (&y)[G * W], float (&u)[G * W], const float (&bias)[W],
                                               const float (&a)[G * W], const float (&b)[G * W], float sD)
 {
     constexpr int E = G * W;
-    const bool want_top = o.amax_out != nullptr || o.out_kind >= OUT_E4M3;
     float value[E], slope[E];
     unsigned top = 0;
     if (OP == OP_ACT || OP == OP_GATED) {
@@ -317,10 +326,8 @@ __device__ __forceinline__ unsigned op_finish(const OpArgs& o, void* D, int64_t 
         act_all<E>(o.act, y, value, slope);
 #pragma unroll
         for (int i = 0; i < E; ++i) value[i] = OP == OP_GATED ? value[i] * u[i] : value[i] + a[i];
-        if (want_top) {
-            zero_outside<G, W>(t, value);
-            top = max_bits_of<E>(value);
-        }
+        zero_outside<G, W>(t, value);
+        top = max_bits_of<E>(value);
         store_rows<G, W>(D, o.out_kind, rows_at(t, N, 0), value, sD, top);
         return top;
     }
@@ -330,16 +337,14 @@ __device__ __forceinline__ unsigned op_finish(const OpArgs& o, void* D, int64_t 
     if (OP == OP_GATED_GRAD) {
 #pragma unroll
         for (int i = 0; i < E; ++i) { value[i] *= y[i]; slope[i] *= b[i]; }
-        if (want_top) {
-            zero_outside<G, W>(t, value);
-            top_u = max_bits_of<E>(value);
-        }
+        zero_outside<G, W>(t, value);
+        top_u = max_bits_of<E>(value);
         store_rows<G, W>(D, o.out_kind, rows_at(t, width, N), value, sD, top_u);
     }
 #pragma unroll
     for (int i = 0; i < E; ++i) y[i] *= slope[i];
-    if (want_top || o.sums) zero_outside<G, W>(t, y);
-    if (want_top) top = max_bits_of<E>(y);
+    zero_outside<G, W>(t, y);
+    top = max_bits_of<E>(y);
     store_rows<G, W>(D, o.out_kind, rows_at(t, width, 0), y, sD, top);
     return max(top, top_u);
 }
@@ -368,6 +373,9 @@ __device__ __forceinline__ void op_commit_top(const OpArgs& o, unsigned bits)
     for (int d = 32; d >= 1; d >>= 1) bits = max(bits, (unsigned)__shfl_xor((int)bits, d, 64));
     if (__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)) == 0) o.tops[blockIdx.x] = bits;
 }
+
+// One value that is the same for all lanes, by the scalar unit: a wait for it is not a wait for the vector loads in flight.
+__device__ __forceinline__ float op_scalar(const float* p) { return *(const __attribute__((address_space(4))) float*)(uintptr_t)p; }
 
 // 1 / the factor of a column of the product (up: of the second projection), in 64 bits: with 1 / sA it is rounded once.
 __device__ __forceinline__ double op_column_factor(const OpArgs& o, int64_t N, int64_t col, bool up)

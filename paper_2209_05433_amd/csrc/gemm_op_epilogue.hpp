@@ -95,9 +95,9 @@ __device__ __forceinline__ void op_store_rows(v16f (&acc)[NB][4], uint8_t* smem,
     double* row_factors = (double*)(smem + OP_ROW_FACTORS) + w * 128;
     double* column_factors = (double*)(smem + OP_COLUMN_FACTORS) + w * 128 + (l % LANES) * (PAIR ? 16 : 8);
     {
-        const double a_all = o.a_per_row ? 1.0 : 1.0 / (double)o.sA_dev[0];
+        const double a_all = o.a_per_row ? 1.0 : 1.0 / (double)op_scalar(o.sA_dev);
         const bool one = o.b_factors == B_ONE;
-        const double b_all = one ? 1.0 / (double)o.sB_dev[0] : 0.0;
+        const double b_all = one ? 1.0 / (double)op_scalar(o.sB_dev) : 0.0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int c = min(col + i, N - 1);
@@ -116,7 +116,12 @@ __device__ __forceinline__ void op_store_rows(v16f (&acc)[NB][4], uint8_t* smem,
 #pragma unroll
         for (int i = 0; i < 2; ++i) *LDS_PTR(double, row_factors + 64 * i + l) = 1.0 / (double)o.sA_dev[min(wave_m0 + 64 * i + l, M - 1)];
     }
-    const float sD = o.out_kind >= OUT_E4M3 ? scale_value(o.sD_dev, 1.0f) : 1.0f;
+    const float sD = o.out_kind >= OUT_E4M3 && o.sD_dev ? op_scalar(o.sD_dev) : 1.0f;
+    // What has been loaded so far is waited for here: at its first use, in the loop, the compiler would wait for all that is in flight, at every trip.
+    if (OP == OP_ACT) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) asm volatile("" : "+v"(bias[i]));
+    }
     float column[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
     unsigned top = 0;
 
@@ -227,11 +232,17 @@ __device__ __forceinline__ void op_store_rows(v16f (&acc)[NB][4], uint8_t* smem,
                     float piece[8];
                     load_row<8>(o.side, o.side_dtype, row * width + col, left, piece);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) a[8 * g + e] = piece[e];
+                    for (int e = 0; e < 8; ++e) {
+                        asm volatile("" : "+v"(piece[e]));      // (waited for on this path, not where the paths meet)
+                        a[8 * g + e] = piece[e];
+                    }
                     if (!BOTH) continue;
                     load_row<8>(o.side, o.side_dtype, row * width + N + col, left, piece);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) b[8 * g + e] = piece[e];
+                    for (int e = 0; e < 8; ++e) {
+                        asm volatile("" : "+v"(piece[e]));
+                        b[8 * g + e] = piece[e];
+                    }
                 }
             }
             finish(in_turn, i, a, b);

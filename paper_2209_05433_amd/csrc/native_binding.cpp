@@ -632,7 +632,7 @@ struct OpProduct {
         nA = fA.numel(); nB = fB.numel();
         sD = is_none(a[at_sD]) ? nullptr : cells(a[at_sD], "the output's factor", 1);
         amax = is_none(a[at_sD + 1]) ? nullptr : cells_out(a[at_sD + 1], "amax_out", 1);
-        fa = small(a[1]); fb = small(a[4]); act = small_of_int(a[10]); flags = small_of_int(a[at_sD + 2]);
+        fa = small(a[1]); fb = small(a[4]); act = small(a[10]); flags = small_of_int(a[at_sD + 2]);
         stream = stream_of(a[at_sD + 3]);
     }
     // A tensor beside the product, of the given number of columns (rows < 0: a vector), or None.

@@ -456,6 +456,69 @@ def test_another_stream_and_graph_replays():
         assert all(torch.equal(a, b) for a, b in zip((H, GU, D, db, top), eager))
 
 
+def test_outputs_that_are_lazy_clones_leave_their_origin_alone():
+    """As for the other entry points (tests/test_gpu_binding.py): every tensor that a call writes gets memory of its own first."""
+    c, wide = Case(64, 32, 96, seed=20), Case(64, 32, 96, wide=True, seed=21)
+    f32 = lambda *s: torch.full(s, 7.0, device="cuda")
+    u8 = lambda *s: torch.full(s, 7, dtype=torch.uint8, device="cuda")
+    Z, GU, norm, act = torch.randn(64, 32, device="cuda"), torch.randn(64, 64, device="cuda"), torch.full((1,), 3.0, device="cuda"), ACTS["silu"]
+    need = fp8.fp8_gemm_act_grad_workspace_size(64, 32)
+    zeros = lambda: torch.zeros(fp8.FP8_GRAD_NORM_WORKSPACE_BYTES, dtype=torch.uint8, device="cuda")
+    calls = {
+        "fp8_gemm_act": ([u8(64, 32), f32(64, 32), f32(1)],
+                         lambda o: fp8.fp8_gemm_act(c.A, E4M3, False, c.B, E4M3, True, o[0], O43, c.sA, c.sB, act, None, None, o[1], None, o[2])),
+        "fp8_gemm_act_grad": ([f32(64, 32), f32(32), u8(need), f32(1)],
+                              lambda o: fp8.fp8_gemm_act_grad(c.A, E4M3, False, c.B, E4M3, True, o[0], F32, c.sA, c.sB, act, Z, o[1], o[2], None, o[3])),
+        "fp8_gemm_gated": ([f32(64, 32), f32(64, 64), f32(1)],
+                           lambda o: fp8.fp8_gemm_gated(wide.A, E4M3, False, wide.B, E4M3, True, o[0], F32, wide.sA, wide.sB, act, o[1], None, o[2])),
+        "fp8_gemm_gated_grad": ([f32(64, 64), f32(1)],
+                                lambda o: fp8.fp8_gemm_gated_grad(c.A, E4M3, False, c.B, E4M3, True, o[0], F32, c.sA, c.sB, act, GU, None, o[1])),
+        "fp8_grad_norm": ([f32(1), zeros()], lambda o: fp8.fp8_grad_norm([Z, GU], o[0], o[1])),
+        "fp8_grad_clip": ([f32(64, 32), f32(64, 64)], lambda o: fp8.fp8_grad_clip([Z, GU], norm, 1.0, o)),
+    }
+    assert set(calls) == set(fp8.binding.OPERATOR_CALLS)
+    for name, (origins, call) in calls.items():
+        before, clones, plain = [t.clone() for t in origins], [torch._lazy_clone(t) for t in origins], [t.clone() for t in origins]
+        call(clones)
+        call(plain)
+        torch.cuda.synchronize()
+        assert all(torch.equal(t, b) for t, b in zip(origins, before)), name
+        assert all(torch.equal(a, b) for a, b in zip(clones, plain)), name
+    x = f32(100)
+    lazy = torch._lazy_clone(x)                              # in place: the clone changes, its origin does not
+    fp8.fp8_grad_clip([lazy], norm, 1.0)
+    torch.cuda.synchronize()
+    assert bool((x == 7.0).all()) and bool((lazy < 7.0).all())
+
+
+def test_arguments_that_do_not_fit():
+    c, D = Case(8, 16, 32, seed=22), torch.empty(8, 16, device="cuda")
+    good = lambda **k: fp8.fp8_gemm_act(**{**dict(A=c.A, fmtA=E4M3, transA=False, B=c.B, fmtB=E4M3, transB=True, D=D, out_kind=F32, sA=c.sA, sB=c.sB, act=0), **k})
+    good()
+    for k in (dict(A=c.A.float()), dict(B=c.B[:, :16]), dict(D=D[:, :8]), dict(D=D.half()), dict(out_kind=BF16), dict(sA=c.sA.double()), dict(bias=torch.zeros(15, device="cuda")),
+              dict(bias=torch.zeros(16)), dict(residual=D.t()), dict(Z=torch.zeros(8, 15, device="cuda")), dict(sD=torch.ones(2, device="cuda"), out_kind=F32), dict(D=torch.empty(8, 32, device="cuda")[:, ::2])):
+        with pytest.raises(ValueError):
+            good(**k)
+    with pytest.raises(TypeError):
+        good(bias=torch.zeros(16, dtype=torch.float16, device="cuda"))
+    with pytest.raises(TypeError):
+        good(act="gelu")
+    for k in (dict(act=7), dict(flags=8), dict(fmtA=3), dict(sD=torch.ones(1, device="cuda"))):
+        with pytest.raises(fp8.Fp8Error) as e:
+            good(**k)
+        assert e.value.status == fp8.FP8_ERR_INVALID_ARG
+    with pytest.raises(ValueError):                          # an odd number of columns for pairs
+        fp8.fp8_gemm_gated(c.A, E4M3, False, c.B[:15].contiguous(), E4M3, True, torch.empty(8, 7, device="cuda"), F32, c.sA, c.sB, 4)
+    with pytest.raises(TypeError):
+        fp8.fp8_gemm_gated_grad(c.A, E4M3, False, c.B, E4M3, True, torch.empty(8, 32, device="cuda"), F32, c.sA, c.sB, 4, None)
+    with pytest.raises(ValueError):
+        fp8.fp8_grad_norm([D], torch.zeros(1, device="cuda"), torch.zeros(64, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(TypeError):
+        fp8.fp8_grad_norm([D.half()], torch.zeros(1, device="cuda"), torch.zeros(1 << 15, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(ValueError):
+        fp8.fp8_grad_clip([D], torch.ones(1, device="cuda"), 1.0, [D.bfloat16()])
+
+
 # ---- norm and clipping of gradients ------------------------------------------------------------------------------------------
 def gradients(sizes, seed, offset=0):
     """Tensors of the given sizes, 16 and 32 bits in turn, each starting at an element of its own choice."""
