@@ -228,9 +228,10 @@ int launch_gemm_op(const GemmArgs& g, const OpArgs& args, float* dbias)
         else if (plan.small == SMALL_32x32 || plan.small == SMALL_32x64) { rows = 32; width = plan.small == SMALL_32x32 ? 32 : 64; }
         auto count = [](int64_t n, int64_t per) { return (n + per - 1) / per; };
         parts = count(g.M, plan.tiled ? rows / 2 : rows);
+        if (o.sums && parts == 1) { o.sums = dbias; dbias = nullptr; }      // one row of partial sums is the sum
         // With a bias gradient there is a launch behind the product anyway: it takes the maxima along, if the workspace has room for them behind the
         // partial sums (4.5 us less than a cell that has to be cleared first).
-        if (o.sums && o.amax_out) {
+        if (dbias && o.amax_out) {
             tops = count(g.M, rows) * (plan.wide_cols ? plan.wide_cols + count(g.N - plan.wide_cols * (int64_t)256, 128) : count(g.N, width));
             if ((count(g.M, kOpSumRows) - parts) * g.N >= tops && tops <= 0x7fffffff) o.tops = (unsigned*)(o.sums + parts * g.N);
         }
