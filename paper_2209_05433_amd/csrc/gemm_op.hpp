@@ -79,10 +79,12 @@ typedef float op_f32x2 __attribute__((ext_vector_type(2)));
 
 // ---- activations ------------------------------------------------------------------------------------------------
 // With s(t) = 1 / (1 + e^-t): SiLU z s(z); GELU z Phi(z); its tanh form z s(2 k (z + 0.044715 z^3)), k = sqrt(2 / pi), since
-// (1 + tanh t) / 2 = s(2 t).  The exponential and the reciprocal are the instructions (1 ulp each).  Phi by Hastings' rational
-// approximation of the error function (Abramowitz and Stegun 7.1.26): with x = |z| / sqrt(2) and t = 1 / (1 + 0.3275911 x) it is
-// 1 - Phi(|z|) = t (a1 + t (a2 + ...)) e^(-x^2) / 2 within 7.5e-8, 20 instruction slots with the derivative's density in them for free (the
-// library's erff: about 100, and 4096 x 6144 outputs spent 15 us a round in it).
+// (1 + tanh t) / 2 = s(2 t).  The exponential and the reciprocal are the instructions (1 ulp each), four slots of the vector ALU each.
+// Phi, where the value alone is asked for: s(z P(z^2)), P fitted to log(Phi(z) / Phi(-z)) / z with degree 6, Phi within 3e-8 over the
+// whole range (beyond the fit z P only grows): 19 slots.  With the derivative, whose density needs e^(-z^2 / 2) anyway, Hastings' rational approximation of
+// the error function (Abramowitz and Stegun 7.1.26): with x = |z| / sqrt(2), t = 1 / (1 + 0.3275911 x)
+// 1 - Phi(|z|) = t (a1 + t (a2 + ...)) e^(-x^2) / 2 within 7.5e-8: 24 slots for the derivative.  (The library's erff: about 100, and 4096 x 6144
+// outputs spent 15 us a round in it.)
 // Beyond |z| = 16 (SiLU: 128) the tails are 0 and 1 in 32 bits; where z would come in as inf x 0 it is held there (a NaN comes through the other
 // factor): act(-inf) is the limit, 0.
 __device__ __forceinline__ float op_sigmoid(float t) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * t)); }
@@ -111,28 +113,51 @@ __device__ __forceinline__ void act_both(float z, float& value, float& slope)
         slope = __builtin_fmaf(__builtin_amdgcn_fmed3f(z, -16.0f, 16.0f) * 0.39894228f, e, p);
     } else {
         const float zc = __builtin_amdgcn_fmed3f(z, -16.0f, 16.0f), q = z == z ? zc * zc : z;
-        const float s = op_sigmoid(1.59576912f * zc * __builtin_fmaf(0.044715f, q, 1.0f));
+        const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(zc * __builtin_fmaf(-0.10294324f, q, -2.3022082f)));
         value = __builtin_amdgcn_fmed3f(z, -16.0f, __builtin_inff()) * s;
         slope = __builtin_fmaf(zc * s * (1.0f - s) * 1.59576912f, __builtin_fmaf(0.134145f, q, 1.0f), s);
     }
 }
 
-template <int E, int ACT>
+// Both GELUs where nobody asks for the derivative; coefficients of -P / log(2), and of -2 k (1 + 0.044715 q) / log(2).
+__device__ __forceinline__ float gelu_value(float z)
+{
+    const float q = z * z;
+    float p = __builtin_fmaf(-5.06754327e-09f, q, 3.81639751e-07f);
+    p = __builtin_fmaf(p, q, -1.14399163e-05f);
+    p = __builtin_fmaf(p, q, 0.00015958029f);
+    p = __builtin_fmaf(p, q, 9.40485625e-05f);
+    p = __builtin_fmaf(p, q, -0.104835123f);
+    p = __builtin_fmaf(p, q, -2.30220938f);
+    return __builtin_amdgcn_fmed3f(z, -16.0f, __builtin_inff()) * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * p));
+}
+__device__ __forceinline__ float gelu_tanh_value(float z)
+{
+    const float p = __builtin_fmaf(-0.10294324f, z * z, -2.3022082f);
+    return __builtin_amdgcn_fmed3f(z, -16.0f, __builtin_inff()) * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * p));
+}
+
+template <int E, int ACT, bool VALUE_ONLY>
 __device__ __forceinline__ void act_each(const float (&z)[E], float (&value)[E], float (&slope)[E])
 {
 #pragma unroll
-    for (int i = 0; i < E; ++i) act_both<ACT>(z[i], value[i], slope[i]);
+    for (int i = 0; i < E; ++i) {
+        if (ACT == FP8_ACT_GELU && VALUE_ONLY) value[i] = gelu_value(z[i]);
+        else if (ACT == FP8_ACT_GELU_TANH && VALUE_ONLY) value[i] = gelu_tanh_value(z[i]);
+        else act_both<ACT>(z[i], value[i], slope[i]);
+    }
 }
 
-template <int E>
+// VALUE_ONLY: slope is not looked at.
+template <int E, bool VALUE_ONLY>
 __device__ __forceinline__ void act_all(int act, const float (&z)[E], float (&value)[E], float (&slope)[E])
 {
     switch (act) {
-        case FP8_ACT_NONE: act_each<E, FP8_ACT_NONE>(z, value, slope); break;
-        case FP8_ACT_RELU: act_each<E, FP8_ACT_RELU>(z, value, slope); break;
-        case FP8_ACT_GELU: act_each<E, FP8_ACT_GELU>(z, value, slope); break;
-        case FP8_ACT_SILU: act_each<E, FP8_ACT_SILU>(z, value, slope); break;
-        default: act_each<E, FP8_ACT_GELU_TANH>(z, value, slope); break;
+        case FP8_ACT_NONE: act_each<E, FP8_ACT_NONE, VALUE_ONLY>(z, value, slope); break;
+        case FP8_ACT_RELU: act_each<E, FP8_ACT_RELU, VALUE_ONLY>(z, value, slope); break;
+        case FP8_ACT_GELU: act_each<E, FP8_ACT_GELU, VALUE_ONLY>(z, value, slope); break;
+        case FP8_ACT_SILU: act_each<E, FP8_ACT_SILU, VALUE_ONLY>(z, value, slope); break;
+        default: act_each<E, FP8_ACT_GELU_TANH, VALUE_ONLY>(z, value, slope); break;
     }
 }
 
@@ -323,7 +348,7 @@ __device__ __forceinline__ unsigned op_finish(const OpArgs& o, void* D, int64_t 
             store_rows<G, W>(o.kept, o.kept_dtype, rows_at(t, OP == OP_GATED ? 2 * N : N, 0), y, 1.0f, 0);
             if (OP == OP_GATED) store_rows<G, W>(o.kept, o.kept_dtype, rows_at(t, 2 * N, N), u, 1.0f, 0);
         }
-        act_all<E>(o.act, y, value, slope);
+        act_all<E, true>(o.act, y, value, slope);
 #pragma unroll
         for (int i = 0; i < E; ++i) value[i] = OP == OP_GATED ? value[i] * u[i] : value[i] + a[i];
         zero_outside<G, W>(t, value);
@@ -331,7 +356,7 @@ __device__ __forceinline__ unsigned op_finish(const OpArgs& o, void* D, int64_t 
         store_rows<G, W>(D, o.out_kind, rows_at(t, N, 0), value, sD, top);
         return top;
     }
-    act_all<E>(o.act, a, value, slope);
+    act_all<E, false>(o.act, a, value, slope);
     const int64_t width = OP == OP_GATED_GRAD ? 2 * N : N;
     unsigned top_u = 0;
     if (OP == OP_GATED_GRAD) {

@@ -319,6 +319,75 @@ def test_tensors_that_start_anywhere(shift):
         run_gated_grad(Case(M, N, K, tB=False, shift=shift, seed=11), "silu", BF16)
 
 
+@pytest.mark.parametrize("name", ["chosen", "small_64x64", "fma"])
+def test_tensors_beyond_32_bits_of_elements(name):
+    """Outputs and the tensors beside them of 2.3e9 elements; the first and the last 300 rows hold something (the other sums are 0)."""
+    M, R, N, K = 140001, 300, 16400, 32
+    F = N // 2
+    ends = (slice(0, R), slice(M - R, M))
+
+    def operands(wide, n, fA, seed):
+        c = Case(R, n, K, fA=fA, wide=wide, seed=seed)
+        A = torch.zeros(M, K, dtype=torch.uint8, device="cuda")
+        for e in ends:
+            A[e] = c.A
+        return c, A
+
+    def beside(c, cols):
+        x = (2 * c.randn(R, cols)).bfloat16()
+        t = torch.zeros(M, cols, dtype=torch.bfloat16, device="cuda")
+        for e in ends:
+            t[e] = x
+        return x.double(), t
+
+    D = torch.empty(M, N, dtype=torch.bfloat16, device="cuda")
+    Z = torch.empty_like(D)
+    with form(name):
+        c, A = operands(False, N, E4M3, 31)
+        r, res = beside(c, N)
+        fp8.fp8_gemm_act(A, E4M3, False, c.B, E4M3, True, D, BF16, c.sA, c.sB, ACTS["gelu"], None, res, Z)
+        want = value(c.c, "gelu") + r
+        for e in ends:
+            accept(D[e], BF16, want, 1.13 * c.E + 2.0 ** -19 * c.c.abs() + 2.0 ** -21 * want.abs(), what="D")
+            accept(Z[e], BF16, c.c, c.E, what="Z")
+        assert not bool(D[M // 2 - 500:M // 2 + 500].any())
+
+        c, A = operands(False, N, E5M2, 32)
+        z, side = beside(c, N)
+        db = torch.empty(N, device="cuda")
+        ws = torch.empty(fp8.fp8_gemm_act_grad_workspace_size(M, N), dtype=torch.uint8, device="cuda")
+        fp8.fp8_gemm_act_grad(A, E5M2, False, c.B, E4M3, True, D, BF16, c.sA, c.sB, ACTS["gelu"], side, db, ws)
+        want = c.c * slope(z, "gelu")
+        err = 1.13 * c.E + 2.0 ** -17 * c.c.abs() + 2.0 ** -21 * want.abs()
+        for e in ends:
+            accept(D[e], BF16, want, err, what="dZ")
+        accept(db, F32, 2 * want.sum(0), 2 * (err.sum(0) + M * 2.0 ** -24 * want.abs().sum(0)), what="dbias")
+        assert not bool(D[M // 2 - 500:M // 2 + 500].any())
+        del side, res
+
+        c, A = operands(True, F, E4M3, 33)
+        H = torch.empty(M, F, dtype=torch.bfloat16, device="cuda")
+        fp8.fp8_gemm_gated(A, E4M3, False, c.B, E4M3, True, H, BF16, c.sA, c.sB, ACTS["silu"], Z)
+        g, u = c.c[:, :F], c.c[:, F:]
+        want = value(g, "silu") * u
+        eg, eu = c.E[:, :F], c.E[:, F:]
+        err = (1.13 * eg + 2.0 ** -19 * g.abs()) * (u.abs() + eu) + value(g, "silu").abs() * eu + 2.0 ** -21 * want.abs()
+        for e in ends:
+            accept(H[e], BF16, want, err, what="H")
+            accept(Z[e], BF16, c.c, c.E, what="GU")
+        del H
+
+        c, A = operands(False, F, E5M2, 34)
+        gu, side = beside(c, N)
+        fp8.fp8_gemm_gated_grad(A, E5M2, False, c.B, E4M3, True, D, BF16, c.sA, c.sB, ACTS["silu"], side)
+        g, u = gu[:, :F], gu[:, F:]
+        want = torch.cat([c.c * u * slope(g, "silu"), c.c * value(g, "silu")], 1)
+        err = torch.cat([u.abs() * (1.13 * c.E + 2.0 ** -17 * c.c.abs()), value(g, "silu").abs() * c.E + 2.0 ** -19 * g.abs() * c.c.abs()], 1) + 2.0 ** -21 * want.abs()
+        for e in ends:
+            accept(D[e], BF16, want, err, what="dGU")
+        assert not bool(D[M // 2 - 500:M // 2 + 500].any())
+
+
 def test_empty_products():
     run_act(Case(5, 0, 16), "gelu", BF16, bias=torch.bfloat16)
     run_act(Case(0, 24, 16), "gelu", BF16, bias=torch.bfloat16)
