@@ -36,14 +36,17 @@ __global__ __launch_bounds__(64 * NW) void gemm_op_skinny_kernel(const uint8_t* 
     for (int p = 0; p < P; ++p) b_row[p] = B + (b_index + p * N) * K;
 
     struct Trip { u32x4 a[PIECES], b[P][PIECES]; };
-    // Beyond the end of K A's piece is zero, and B's one of the same row (whatever it holds: a NaN there is in the sum anyway).
+    // Beyond the end of K A's piece is zero, and B's the row's last one, where no infinity (0 x inf) can be: a NaN there is in the sum anyway.
     auto fetch = [&](Trip& t, int64_t trip) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             const int64_t k = trip * (64 * PIECES) + 64 * i + 16 * g, at = k < K ? k : K - 16;
             t.a[i] = *(const u32x4*)(a_row + at);
 #pragma unroll
-            for (int p = 0; p < P; ++p) t.b[p][i] = *(const u32x4*)(b_row[p] + at);
+            for (int p = 0; p < P; ++p) {
+                t.b[p][i] = *(const u32x4*)(b_row[p] + at);
+                if (FMT_B == FP8_E5M2 && k >= K) t.b[p][i] = (u32x4){0u, 0u, 0u, 0u};
+            }
             if (k >= K) t.a[i] = (u32x4){0u, 0u, 0u, 0u};
         }
     };

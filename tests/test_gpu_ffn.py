@@ -474,6 +474,27 @@ def test_nan_and_infinity(name):
 
 
 @pytest.mark.parametrize("name", list(FORMS))
+@pytest.mark.parametrize("M", [3, 70])
+def test_an_infinity_at_the_end_of_k_gives_infinite_sums(M, name):
+    """K = 272 fills no chunk, trip or stage: what stands in for the rest has to leave the sums alone."""
+    N, K = 48, 272
+    for tB in (True, False):
+        c = Case(M, N, K, tB=tB, fA=E5M2, fB=E5M2, seed=12)
+        c.A[:, K - 1] = 0x3C                                    # 1.0 against the infinity
+        (c.B[5] if tB else c.B[:, 5])[K - 1] = 0x7C
+        want = torch.zeros(M, N, dtype=torch.bool, device="cuda")
+        want[:, 5] = True
+        D = torch.empty(M, N, device="cuda")
+        G = torch.empty(M, N // 2, device="cuda")
+        GU = torch.empty(M, N, device="cuda")
+        with form(name):
+            fp8.fp8_gemm_act(c.A, E5M2, False, c.B, E5M2, tB, D, F32, c.sA, c.sB, ACTS["none"])
+            fp8.fp8_gemm_gated(c.A, E5M2, False, c.B, E5M2, tB, G, F32, c.sA, c.sB, ACTS["none"], GU)
+        assert torch.equal(D == float("inf"), want) and torch.equal(D.isfinite(), ~want)
+        assert torch.equal(GU == float("inf"), want) and torch.equal(GU.isfinite(), ~want)
+
+
+@pytest.mark.parametrize("name", list(FORMS))
 def test_sums_are_the_same_in_every_run(name):
     c = Case(500, 272, 512, tB=False, seed=9)
     runs = []
