@@ -8,7 +8,8 @@
 // The tensors, up to a few hundred a launch, come in the kernel's arguments (no table in device memory that somebody would have to copy
 // and keep); they are cut into chunks of kChunk elements, which a grid of at most kMostBlocks workgroups walks.  Bound by memory: 2 or 4
 // bytes read an element for the norm, as many read and written for the clipping.  The clipping walks the chunks from the last to the
-// first: what the norm has read last is still in the last-level cache.  2 GB of bf16: the norm at 6.2 TB/s, the clipping at 6.3.
+// first: what the norm has read last is still in the last-level cache.  2 GB of bf16: the norm at 5.7 TB/s (355 us), the clipping at
+// 6.2 (650).  An empty tensor or a single one costs a search over the list, per chunk, that other workgroups hide (chunks one behind the other: 360).
 #include "gemm_common.hpp"
 
 #include <algorithm>
