@@ -217,6 +217,16 @@ __device__ __forceinline__ void each_row(const RowsAt<G>& t, F store)
     }
 }
 
+// A lane's columns of a row.  At a tile's end (several rows at a time) the waves write whole lines, which push no operands out of the caches: 4096 x 6144
+// x 2048 114.7 -> 113.2 us, 8192 x 6144 gradients of a gated block 229.4 -> 227.1, 1537 x 5504 67.0 -> 65.2; with the product that reads the output behind
+// them 203 -> 200 and 289.5 -> 288.5, the gated block of 8192 rows 494 -> 484, of 300 rows 53.8 -> 54.0.
+template <int G, class V> __device__ __forceinline__ void store_columns(void* p, V v)
+{
+    typedef V any __attribute__((aligned(1)));
+    if (G > 1) __builtin_nontemporal_store(v, (any*)p);
+    else *(any*)p = v;
+}
+
 // out_kind: as of a product's output (the first two are fp8_dtype_t); sD: of FP8 kinds, max_bits: the largest magnitude of v there, as bits.
 template <int G, int W>
 __device__ __forceinline__ void store_rows(void* p, int out_kind, const RowsAt<G>& t, const float (&v)[G * W], float sD, unsigned max_bits)
@@ -229,8 +239,8 @@ __device__ __forceinline__ void store_rows(void* p, int out_kind, const RowsAt<G
             unsigned short* h = (unsigned short*)p + t.at[g];
             const unsigned* r = x + g * (W / 2);
             if (t.whole || t.left >= W) {
-                if (W == 8) *(u32x4_any*)h = (u32x4){r[0], r[1], r[W / 2 - 2], r[W / 2 - 1]};
-                else *(u32x2_any*)h = (u32x2){r[0], r[1]};
+                if (W == 8) store_columns<G>(h, (u32x4){r[0], r[1], r[W / 2 - 2], r[W / 2 - 1]});
+                else store_columns<G>(h, (u32x2){r[0], r[1]});
             } else {
 #pragma unroll
                 for (int i = 0; i < W - 1; ++i) if (i < t.left) h[i] = (unsigned short)(r[i >> 1] >> (16 * (i & 1)));
@@ -243,7 +253,7 @@ __device__ __forceinline__ void store_rows(void* p, int out_kind, const RowsAt<G
             if (t.whole || t.left >= W) {
 #pragma unroll
                 for (int i = 0; i < W / 4; ++i)
-                    *(u32x4_any*)(f + 4 * i) = (u32x4){as_u32(r[4 * i]), as_u32(r[4 * i + 1]), as_u32(r[4 * i + 2]), as_u32(r[4 * i + 3])};
+                    store_columns<G>(f + 4 * i, (u32x4){as_u32(r[4 * i]), as_u32(r[4 * i + 1]), as_u32(r[4 * i + 2]), as_u32(r[4 * i + 3])});
             } else {
 #pragma unroll
                 for (int i = 0; i < W - 1; ++i) if (i < t.left) f[i] = r[i];
@@ -283,8 +293,8 @@ __device__ __forceinline__ void store_rows(void* p, int out_kind, const RowsAt<G
             uint8_t* q = (uint8_t*)p + t.at[g];
             const unsigned* r = x + g * (W / 4);
             if (t.whole || t.left >= W) {
-                if (W == 8) *(u32x2_any*)q = (u32x2){r[0], r[W / 4 - 1]};
-                else *(unsigned __attribute__((aligned(1)))*)q = r[0];
+                if (W == 8) store_columns<G>(q, (u32x2){r[0], r[W / 4 - 1]});
+                else store_columns<G>(q, r[0]);
             } else {
 #pragma unroll
                 for (int i = 0; i < W - 1; ++i) if (i < t.left) q[i] = (uint8_t)(r[i >> 2] >> (8 * (i & 3)));

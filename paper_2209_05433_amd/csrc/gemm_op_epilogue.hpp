@@ -18,7 +18,7 @@ namespace {
 // One wave a SIMD, nothing hides a load from memory.  What is read beside the product (z, g | u, the residual) therefore goes from
 // memory straight into a ring in LDS, several steps ahead, a lane's 16 bytes where the same lane reads them; waits are counted by hand.  (As loads
 // into registers the compiler waited for all of them at the first: its counts do not survive the branches around the stores.
-// 8192 x 6144 gradients of a gated block with K = 2048: 343 us unasked, 267 in registers, 233 to 241 in the ring, the waits and the arithmetic around it put right; the
+// 8192 x 6144 gradients of a gated block with K = 2048: 343 us unasked, 267 in registers, 260 in the ring, 227 with no uncounted wait left; the
 // product alone, to bf16, 170.)
 constexpr int OP_RING = 69 * 1024, OP_RING_WAVE = 20 * 1024;            // LDS behind the turned rows: the waves' rings
 constexpr int OP_ROW_FACTORS = 149 * 1024, OP_COLUMN_FACTORS = 153 * 1024, OP_AMAX = 157 * 1024;        // reciprocals of factors; a word per wave
