@@ -298,6 +298,17 @@ def test_larger_products_by_the_librarys_choice(M, N, K):
         run_gated_grad(Case(M, N, K, tB=False, fA=E5M2, flags=flags, seed=4), "silu", O52)
 
 
+@pytest.mark.parametrize("name", ["chosen", "tiled_256", "tiled_128", "tiled_both"])
+@pytest.mark.parametrize("M,N,K", [(272, 144, 100), (528, 272, 333), (256, 512, 33), (16, 32, 129)])
+def test_any_k_where_no_operand_is_contiguous_along_it(M, N, K, name):
+    for flags in (0, fp8.FP8_GEMM_MFMA8):
+        order = dict(tA=True, tB=False, flags=flags)
+        run_act(Case(M, N, K, seed=21, **order), "gelu", BF16, bias=torch.float32, residual=torch.bfloat16, name=name)
+        run_act_grad(Case(M, N, K, fA=E5M2, seed=22, **order), "silu", O52, name=name)
+        run_gated(Case(M, N, K, wide=True, seed=23, **order), "silu", O43, name=name)
+        run_gated_grad(Case(M, N, K, fA=E5M2, seed=24, **order), "gelu", F32, gu=torch.float32, name=name)
+
+
 @pytest.mark.parametrize("name", list(FORMS))
 def test_in_place(name):
     """The residual, z or g | u where the output goes."""
