@@ -447,6 +447,7 @@ int fp8_gemm_act_grad(const uint8_t* A, int fmtA, int transA, const uint8_t* B, 
  *   H    device, M x F of out_kind
  *   sB_dev  nsB values: 1, 2 (of the gate, of the other projection) or 2F (one per column of op(B))
  *   GU   device, M x 2F of GU_dtype, or NULL: what the backward pass needs
+ *   flags   as for fp8_gemm_act; with B given as K x 2F, F has to be a multiple of 16 for the FP8 instructions
  * The rest as for fp8_gemm_act.
  */
 int fp8_gemm_gated(const uint8_t* A, int fmtA, int transA, const uint8_t* B, int fmtB, int transB,

@@ -165,14 +165,17 @@ OpPlan plan_op(const GemmArgs& g, const OpArgs& o)
     if (chosen && op_skinny_takes(g, pair)) return {false, false, SMALL_NONE, (int)ACC_F16, 0, 0, true};
     const GemmPlan plan = plan_gemm(p, false);
     if (plan.kernel == GEMM_GENERIC) return plain_fmas;
-    if (plan.small != SMALL_NONE) return {false, false, plan.small, g.acc, 0, 0, false};
+    // Shapes and alignments outside the tiled kernel's, and any K that is no multiple of 16, are computed on the fp16 instructions, whatever the flag
+    // says: callers are promised fp8_gemm's bound there.  (Of a gated block F is what has to be a multiple of 16, not 2 F.)
+    const bool halves = !pair || g.transB || g.N % 16 == 0;
+    const int acc = plan.kernel == GEMM_MFMA_ANY || !halves || g.K % 16 ? (int)ACC_F16 : g.acc;
+    if (plan.small != SMALL_NONE) return {false, false, plan.small, acc, 0, 0, false};
     // The tiled kernel exists for a weight in E4M3 (the format of weights); E5M2, and shapes and alignments that it does not take, go to tiles of 64 x 64 (4096 x 6144 x
     // 2048 with GELU 108 us, in E5M2 171; with K = 2047 226; up to some hundreds of tiles as fast as the plain product).
-    const bool tiled = plan.kernel != GEMM_MFMA_ANY && g.fmtB == FP8_E4M3 && (!pair || (g.transB ? (uint64_t)(g.N + TILE_M) * (uint64_t)g.K < (1ull << 32) : g.N % 16 == 0));
-    if (!tiled) return ((g.M + 63) / 64) * ((p.N + 63) / 64) > 0x7fffffffll ? plain_fmas : OpPlan{false, false, SMALL_64x64, g.acc, 0, 0, false};
+    const bool tiled = plan.kernel != GEMM_MFMA_ANY && g.fmtB == FP8_E4M3 && halves && (!pair || !g.transB || (uint64_t)(g.N + TILE_M) * (uint64_t)g.K < (1ull << 32));
+    if (!tiled) return ((g.M + 63) / 64) * ((p.N + 63) / 64) > 0x7fffffffll ? plain_fmas : OpPlan{false, false, SMALL_64x64, acc, 0, 0, false};
     // The width whose rounds of 256 workgroups take less time, or both widths in one launch, by the plain product's model of run times with the
     // operator's own time on top (us of a 256-wide tile: fitted to 8192 x 8192 outputs over K = 256; it is the same per output in both widths).
-    const int acc = g.K % 16 ? (int)ACC_F16 : g.acc;
     const TileTimes t = tile_times(acc, 2.0 * (double)((g.K + 2 * TILE_K - 1) / (2 * TILE_K)));
     const double own = o.op == OP_GATED_GRAD ? 25.0 : o.op == OP_GATED ? 3.0 : o.op == OP_ACT_GRAD || o.side ? 12.0 : 7.0;
     const double wide = t.wide + own, narrow = t.narrow + 0.5 * own;
