@@ -480,7 +480,7 @@ int fp8_gemm_gated_grad(const uint8_t* A, int fmtA, int transA, const uint8_t* B
  *   out        out[i] has x[i]'s type; NULL, or out[i] = x[i]: in place.  Other overlaps are not allowed.
  *   norm       device, one fp32 (what fp8_grad_norm wrote)
  *   max_norm   a number >= 0
- * An infinite norm makes the factor 0, a NaN norm makes every output NaN.  Tensors of no elements may have NULL pointers.
+ * An infinite norm makes the factor 0 whatever max_norm (infinity: no bound), a NaN norm makes every output NaN.  Tensors of no elements may have NULL pointers.
  */
 #define FP8_GRAD_NORM_WORKSPACE_BYTES 32768
 int fp8_grad_norm(int count, const void* const* x, const size_t* n, const int* dtype, float* norm_out, void* workspace, void* stream);

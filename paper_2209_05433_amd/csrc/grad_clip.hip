@@ -202,8 +202,10 @@ __device__ __forceinline__ void scale_chunk(const void* x, void* out, unsigned c
 template <bool STREAM>
 __global__ __launch_bounds__(kThreads) void grad_clip_kernel(ClipTensors list, unsigned chunks, const float* norm, float max_norm, bool in_place)
 {
-    float f = max_norm / (*norm + 1e-6f);
+    const float n = *norm;
+    float f = max_norm / (n + 1e-6f);
     if (f > 1.0f) f = 1.0f;                      // (NaN stays)
+    if (n == __builtin_inff()) f = 0.0f;         // (also where max_norm is infinite)
     if (in_place && f == 1.0f) return;           // x 1 = x
     for (unsigned c = blockIdx.x; c < chunks; c += gridDim.x) {
         // the list begins with the last tensor; its chunks from the last one on
