@@ -195,6 +195,10 @@ __device__ __forceinline__ void direct_load_or_zero(const uint8_t* base, unsigne
     asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" :: "v"(p), "{m0}"(lds_addr) : "memory");
 }
 
+// The output of the plain product is nobody else's memory; an operator may read there what it replaces (the residual, z, g | u).
+template <int OP> struct TileOutput { typedef void* type; };
+template <> struct TileOutput<0> { typedef void* __restrict__ type; };
+
 // A_KC / B_KC: how the operand lies in memory (see Operand); NB: width of the tile in blocks of 32
 // columns per wave.  LDS: an MN-contiguous operand takes a ring of four stage slabs; a K-contiguous
 // one a ring of three stage-pair slabs, or of two for B when both operands are K-contiguous.
@@ -219,7 +223,7 @@ __device__ __forceinline__ void direct_load_or_zero(const uint8_t* base, unsigne
 // is tiles_n tiles wide (the whole output for the plain kernel; see gemm_mixed_kernel).
 template <int FMT_A, int FMT_B, int ACC, bool A_KC, bool B_KC, int NB, bool PERSIST, int OP = 0>
 __device__ __forceinline__ void gemm_tile_body(
-    const uint8_t* __restrict__ A, const uint8_t* __restrict__ B, void* __restrict__ C,
+    const uint8_t* __restrict__ A, const uint8_t* __restrict__ B, typename TileOutput<OP>::type C,
     int M, int N, int K, const EpilogueArgs& ep, int group_m, int splits, int pairs_per_split,
     int bid_in, int n_begin, int tiles_n)
 {
