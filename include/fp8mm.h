@@ -429,8 +429,8 @@ int fp8_gemm_act(const uint8_t* A, int fmtA, int transA, const uint8_t* B, int f
  * (A: the gradient of the next layer's output, B: that layer's weight.)
  *   Z          device, M x N of Z_dtype, as fp8_gemm_act kept it; may be D itself where the types are the same
  *   dbias      device, N fp32 values, or NULL.  Written, not accumulated; sums of y in 32 bits, in the same order in every run.
- *   workspace  device, 4-byte aligned, at least fp8_gemm_act_grad_workspace_size(M, N) bytes = 4 N for every 32 rows; contents on
- *              entry are irrelevant.  Only looked at where dbias is given.
+ *   workspace  device, 4-byte aligned, at least fp8_gemm_act_grad_workspace_size(M, N) bytes = 4 N for every 32 rows (or
+ *              SIZE_MAX, if a size_t holds no such number); contents on entry are irrelevant.  Only looked at where dbias is given.
  */
 size_t fp8_gemm_act_grad_workspace_size(int64_t M, int64_t N);
 int fp8_gemm_act_grad(const uint8_t* A, int fmtA, int transA, const uint8_t* B, int fmtB, int transB,

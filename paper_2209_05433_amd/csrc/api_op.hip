@@ -105,7 +105,9 @@ int fp8_gemm_act(const uint8_t* A, int fmtA, int transA, const uint8_t* B, int f
 
 size_t fp8_gemm_act_grad_workspace_size(int64_t M, int64_t N)
 {
-    return M <= 0 || N <= 0 ? 0 : (size_t)((M + kOpSumRows - 1) / kOpSumRows) * (size_t)N * 4;
+    if (M <= 0 || N <= 0) return 0;
+    const size_t rows = (size_t)(M - 1) / kOpSumRows + 1;
+    return rows > SIZE_MAX / 4 / (size_t)N ? SIZE_MAX : rows * (size_t)N * 4;
 }
 
 int fp8_gemm_act_grad(const uint8_t* A, int fmtA, int transA, const uint8_t* B, int fmtB, int transB, void* D, int out_kind, int64_t M, int64_t N, int64_t K,
