@@ -150,7 +150,8 @@ __global__ __launch_bounds__(256) void column_sum_kernel(const float* __restrict
     if (w == 0 && col < N) dbias[col] = (part[0][l] + part[1][l]) + (part[2][l] + part[3][l]);
 }
 
-// Which kernel takes the call, as for the plain product of the same operands.
+// Which kernel takes the call: the one of few rows where it pays, else what the plain product of the same operands takes, as far as it exists with these ends
+// (not the any-shape kernel, tiles of 192 columns or the persistent form).
 struct OpPlan { bool generic, tiled; int small, acc, tile_n, wide_cols; bool skinny; };
 OpPlan plan_op(const GemmArgs& g, const OpArgs& o)
 {

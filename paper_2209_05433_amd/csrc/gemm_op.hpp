@@ -35,7 +35,6 @@ struct OpArgs : EpilogueArgs {                  // (sA_dev, sB_dev: given; b_per
 
 constexpr int kOpSumRows = 32;                  // rows of the output behind one row of partial column sums, at least
 inline bool op_pair_in(int op) { return op == OP_GATED; }             // B has two columns for each output column
-inline int64_t op_width(int op, int64_t N) { return op == OP_GATED_GRAD ? 2 * N : N; }
 
 // g: operands, D, M, N (columns of D, or of either half), K; g.ep is not looked at.
 int launch_gemm_op(const GemmArgs& g, const OpArgs& o, float* dbias);
@@ -80,11 +79,15 @@ typedef float op_f32x2 __attribute__((ext_vector_type(2)));
 // ---- activations ------------------------------------------------------------------------------------------------
 // With s(t) = 1 / (1 + e^-t): SiLU z s(z); GELU z Phi(z); its tanh form z s(2 k (z + 0.044715 z^3)), k = sqrt(2 / pi), since
 // (1 + tanh t) / 2 = s(2 t).  The exponential and the reciprocal are the instructions (1 ulp each), four slots of the vector ALU each.
-// Phi, where the value alone is asked for: s(z P(z^2)), P fitted to log(Phi(z) / Phi(-z)) / z with degree 6, Phi within 3e-8 over the
-// whole range (beyond the fit z P only grows): 19 slots.  With the derivative, whose density needs e^(-z^2 / 2) anyway, Hastings' rational approximation of
-// the error function (Abramowitz and Stegun 7.1.26): with x = |z| / sqrt(2), t = 1 / (1 + 0.3275911 x)
-// 1 - Phi(|z|) = t (a1 + t (a2 + ...)) e^(-x^2) / 2 within 7.5e-8: 24 slots for the derivative.  (The library's erff: about 100, and 4096 x 6144
+// Phi, where the value alone is asked for: s(z P(z^2)), P fitted to log(Phi(z) / Phi(-z)) / z with degree 6, Phi within 3.7e-8 over the
+// whole range (beyond the fit z P only grows) but for rounding: 19 slots.  With the derivative, whose density needs e^(-z^2 / 2) anyway, Hastings' rational
+// approximation of the error function (Abramowitz and Stegun 7.1.26): with x = |z| / sqrt(2), t = 1 / (1 + 0.3275911 x)
+// 1 - Phi(|z|) = t (a1 + t (a2 + ...)) e^(-x^2) / 2 within 7.5e-8 but for rounding: 24 slots for the derivative.  (The library's erff: about 100, and 4096 x 6144
 // outputs spent 15 us a round in it.)
+// Measured at 4 million z between -20 and 31, |error| / |z| of the value at most 1.7e-7 (GELU), 1.5e-7 (its tanh form, SiLU), GELU's beside its
+// derivative 3.0e-7; of the derivative 3.1e-7 (GELU), 2.0e-6 (tanh form), 9.8e-7 (SiLU).  GELU's bounds are absolute: of its left tail little
+// is right beyond z = -5 (a value of 1e-6), by 1.4e-5 of the value at -3, 1 % at -5, 94 % at -6, as of (1 + erf) / 2 in 32 bits, where 1 + erf cancels.
+// The other two keep their digits there.
 // Beyond |z| = 16 (SiLU: 128) the tails are 0 and 1 in 32 bits; where z would come in as inf x 0 it is held there (a NaN comes through the other
 // factor): act(-inf) is the limit, 0.
 __device__ __forceinline__ float op_sigmoid(float t) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * t)); }
