@@ -490,6 +490,81 @@ int fp8_grad_clip(int count, const void* const* x, const size_t* n, const int* d
                   float max_norm, void* stream);
 
 /*
+ * ---- The two ends of a training step -------------------------------------------------------------------
+ *
+ * fp8_gemm_xent -- softmax cross entropy over a vocabulary, behind the product that makes the logits, which are in no memory at any time:
+ *     z_ij   = (sum_k a_ik b_kj) / (sA_i * sB_j)
+ *     lse_i  = log sum_j exp(z_ij)
+ *     loss_i = lse_i - z_i,y(i) + z_weight * lse_i^2,  y(i) = labels_i - first;  0 for a row without a label
+ *   A, B, factors, M, N, K, flags  as for fp8_gemm_fused (A: the tokens' hidden vectors, B: the vocabulary's weight)
+ *   labels     device, M values of 64 bits.  Negative: the row has no label (padding, a prompt): its loss is 0, its lse is written all the same.
+ *   first      which label the first column stands for: columns are a piece of the vocabulary, [first, first + N).  Of a label outside the
+ *              piece no z is taken: loss_i = lse_i + z_weight * lse_i^2.  (Pieces, here or on other GPUs, without z_weight: lse = log sum exp(lse of
+ *              each), loss = lse + sum of (loss - lse of each).)
+ *   z_weight   a finite number >= 0
+ *   loss, lse  device, M fp32 values each
+ *   workspace  device, 8-byte aligned, at least fp8_gemm_xent_workspace_size(M, N) bytes = 8 M (ceil(N / 32) + 1) (SIZE_MAX, if a size_t holds no
+ *              such number); contents on entry are irrelevant; calls that may overlap need workspaces of their own
+ * z_ij meets the bound of fp8_gemm (fp8_gemm_mfma8 with FP8_GEMM_MFMA8).  Sums of exponentials are held in 32 bits around the row's maximum in each run of up to
+ * 128 columns and joined in 64: beyond what the z_ij are off by, lse is within 2^-22 (|lse| + max |z|) + 2^-20.  Results are the same in every run.
+ * Logits of -infinity count nothing (all of them: lse = -infinity); +infinity makes lse +infinity, NaN makes it NaN.
+ */
+size_t fp8_gemm_xent_workspace_size(int64_t M, int64_t N);
+int fp8_gemm_xent(const uint8_t* A, int fmtA, int transA, const uint8_t* B, int fmtB, int transB, int64_t M, int64_t N, int64_t K,
+                  const float* sA_dev, int64_t nsA, const float* sB_dev, int64_t nsB, const int64_t* labels, int64_t first, float z_weight,
+                  float* loss, float* lse, void* workspace, size_t workspace_bytes, int flags, void* stream);
+
+/*
+ * fp8_gemm_xent_grad -- the gradient of the loss with respect to the logits, which are computed once more:
+ *     y_ij = dloss_i * (exp(z_ij - lse_i) (1 + 2 z_weight lse_i) - [first + j = labels_i]);  0 in a row without a label, whatever its z
+ *     D_ij = cast_out(y_ij), or encode(fl32(y_ij * sD)) for FP8 kinds;  amax = max |y_ij|
+ * D (E5M2 as a rule: |y_ij| <= |dloss_i| without z_weight, which is what sD can be chosen by) is the operand of the products for the tokens' gradient (D times the
+ * vocabulary's weight) and the weight's (D transposed times the tokens).  A vocabulary that is taken in pieces needs D for one piece at a time:
+ * B the piece's rows of the weight, N their number, first the first one; fp8_gemm_act with the residual in place adds up the tokens' gradient.
+ *   lse     device, M fp32 values: of the whole vocabulary, as fp8_gemm_xent leaves them
+ *   dloss   device, ndloss fp32 values: the gradient of each row's loss (ndloss = M) or of all (1)
+ *   D, out_kind, sD_dev, amax_out  as for fp8_gemm_fused.  D must not overlap any other argument.
+ * The rest as for fp8_gemm_xent.  Beyond what z_ij is off by, the exponential is within 2^-22 (|z_ij| + |lse_i| + 4) of itself.
+ */
+int fp8_gemm_xent_grad(const uint8_t* A, int fmtA, int transA, const uint8_t* B, int fmtB, int transB, void* D, int out_kind, int64_t M, int64_t N, int64_t K,
+                       const float* sA_dev, int64_t nsA, const float* sB_dev, int64_t nsB, const int64_t* labels, int64_t first, float z_weight,
+                       const float* lse, const float* dloss, int64_t ndloss, const float* sD_dev, float* amax_out, int flags, void* stream);
+
+/*
+ * fp8_adamw -- one step of AdamW on `count` tensors, with the gradients' clipping, states in 32 bits or in FP8, and the new weights in FP8:
+ *     g  = grad * min(1, max_norm / (norm + 1e-6))           (norm given; as fp8_grad_clip, nothing is written to grad)
+ *     m' = beta1 m + (1 - beta1) g;   v' = beta2 v + (1 - beta2) g^2
+ *     p' = p - lr (weight_decay p + (m' / (1 - beta1^t)) / (sqrt(v' / (1 - beta2^t)) + eps)),  t = *step
+ *     q  = encode(fl32(p' * q_scale)),  q_amax = max |p'|     (p' before it is rounded to p's type)
+ * p, g, m, v, m_scale, v_scale, q, n, p_dtype, g_dtype and weight_decay are HOST arrays of `count` entries (read before the call returns).  p, m, v are updated in
+ * place.  Tensors are contiguous and may start anywhere their element may; no two may overlap, and none may be in the list twice.
+ *   p, p_dtype  the weights, n[i] elements, fp8_dtype_t; g, g_dtype: their gradients
+ *   state_kind  FP8_STATE_F32: m[i], v[i] are n[i] fp32 values.
+ *               FP8_STATE_FP8: n[i] bytes of E4M3 each, of m and of sqrt(v), and m_scale[i], v_scale[i] ceil(n[i] / 128) fp32 factors, one for each 128 elements:
+ *               m = decode(byte) / factor.  A state of zeros is bytes 0 and factors 1.  The step leaves factors of 448 over the block's largest magnitude (1 where
+ *               that is 0 or not finite) and bytes rounded stochastically as by fp8_quantize_sr: to the neighbour above where T + r >= 2^16; r of m the low, of sqrt(v)
+ *               the high half of word e % 4 of Philox4x32-10 with the counter (e / 4: two words, t's low word, i) and the key `seed`, e: the element, i: the tensor.
+ *               A positive sqrt(v) never becomes 0.  Factors that are not finite and > 0 are not a state.
+ *   seed        of FP8 states; one for a whole run of training will do
+ *   weight_decay  finite numbers >= 0, or NULL: none
+ *   lr, step    device: one fp32, one int64 >= 1 (the caller counts)
+ *   beta1, beta2  in [0, 1);  eps: a finite number >= 0
+ *   norm        device, one fp32 (what fp8_grad_norm wrote), or NULL: no clipping;  max_norm: a number >= 0, not looked at without norm
+ *   q           NULL, or n[i] bytes or NULL for each tensor: FP8 copies in q_fmt (fp8_format_t), saturating
+ *   q_scale     device, `count` fp32 factors (of tensors without a copy not looked at); needed with q
+ *   q_amax      device, `count` fp32 values, or NULL.  Written, not accumulated; 0 of tensors without a copy
+ *   flags       FP8_ADAMW_SKIP_NONFINITE: an infinite or NaN norm leaves everything as it is (else as for fp8_grad_clip)
+ * Computed in 32 bits, m', v' rounding every sum and product once.  Results are the same in every run.
+ */
+typedef enum { FP8_STATE_F32 = 0, FP8_STATE_FP8 = 1 } fp8_state_t;
+#define FP8_ADAMW_SKIP_NONFINITE 1
+#define FP8_STATE_BLOCK 128
+int fp8_adamw(int count, void* const* p, const int* p_dtype, const void* const* g, const int* g_dtype, const size_t* n, void* const* m, void* const* v,
+              int state_kind, float* const* m_scale, float* const* v_scale, uint64_t seed, const float* weight_decay, const float* lr, const int64_t* step,
+              double beta1, double beta2, float eps, const float* norm, float max_norm, uint8_t* const* q, int q_fmt, const float* q_scale, float* q_amax,
+              int flags, void* stream);
+
+/*
  * Which kernel the GEMM entry points would run for a problem, small ones apart (diagnostics; nothing is launched and
  * no pointer is dereferenced: only shapes, storage orders and pointer alignment decide).  Pass the
  * pointers of the intended call; sB_per_column is the per-column factor vector of fp8_gemm_fused or

@@ -28,10 +28,13 @@ UNITS = [("gemm_tiled.hip", ["-DFP8MM_LAYOUT=%d" % k, "-DFP8MM_ACC=%d" % a], "ge
         [("gemm_op_tiled.hip", ["-DFP8MM_LAYOUT=%d" % k, "-DFP8MM_ACC=%d" % a], "gemm_op_tiled_l%d_a%d.o" % (k, a))
          for k in range(4) for a in range(2)] + \
         [("gemm_op_small.hip", ["-DFP8MM_LAYOUT=%d" % k], "gemm_op_small_l%d.o" % k) for k in range(4)] + \
+        [("gemm_op_tiled.hip", ["-DFP8MM_LAYOUT=%d" % k, "-DFP8MM_ACC=%d" % a, "-DFP8MM_LOSS"], "gemm_loss_tiled_l%d_a%d.o" % (k, a))
+         for k in range(2) for a in range(2)] + \
+        [("gemm_op_small.hip", ["-DFP8MM_LAYOUT=%d" % k, "-DFP8MM_LOSS"], "gemm_loss_small_l%d.o" % k) for k in range(4)] + \
         [("gemm_dispatch.hip", [], "gemm_dispatch.o"), ("gemm_splitk.hip", [], "gemm_splitk.o"),
          ("cast_kernels.hip", [], "cast_kernels.o"),
          ("cast_variants.hip", [], "cast_variants.o"),
-         ("gemm_op.hip", [], "gemm_op.o"), ("gemm_op_skinny.hip", [], "gemm_op_skinny.o"), ("grad_clip.hip", [], "grad_clip.o"), ("api_op.hip", [], "api_op.o"),
+         ("gemm_op.hip", [], "gemm_op.o"), ("gemm_op_skinny.hip", [], "gemm_op_skinny.o"), ("grad_clip.hip", [], "grad_clip.o"), ("gemm_loss.hip", [], "gemm_loss.o"), ("adamw.hip", [], "adamw.o"), ("api_op.hip", [], "api_op.o"),
          ("api.hip", [], "api.o")]
 
 # -packed-fp32-ops is switched off on purpose: the compiler must not form packed fp32

@@ -1,5 +1,10 @@
-// extern "C" entry points of the feed-forward operators: argument validation, then one launcher each.
-#include "gemm_op.hpp"
+// extern "C" entry points of the feed-forward operators, the loss over a vocabulary and AdamW: argument validation, then one launcher each.
+#include "gemm_loss.hpp"
+
+#include <algorithm>
+#include <exception>
+#include <utility>
+#include <vector>
 
 using namespace fp8mm;
 
@@ -40,11 +45,20 @@ int fill_op(const char* who, GemmArgs& g, OpArgs& o, int op, const uint8_t* A, i
     g.transA = transA != 0; g.transB = transB != 0; g.acc = (flags & FP8_GEMM_MFMA8) ? ACC_FP8 : ACC_F16;
     g.splits = 1;
     g.stream = (hipStream_t)stream;
-    o = OpArgs{};
     o.sA_dev = sA_dev; o.sB_dev = sB_dev; o.sD_dev = sD_dev; o.amax_out = amax_out;
     o.op = op; o.act = act; o.out_kind = out_kind;
     o.a_per_row = nsA == M && M != 1;
     o.b_factors = nsB == 1 ? B_ONE : pair ? B_PAIR : B_COLUMN;
+    return FP8_OK;
+}
+
+// What the loss and its gradient share beyond that.
+int fill_loss(const char* who, LossArgs& o, int64_t M, const int64_t* labels, int64_t first, float z_weight)
+{
+    if (M > 0 && (!labels || (uintptr_t)labels % 8)) return fail(FP8_ERR_INVALID_ARG, "%s: labels is NULL or misaligned", who);
+    if (first < 0) return fail(FP8_ERR_INVALID_ARG, "%s: first = %lld is negative", who, (long long)first);
+    if (!(z_weight >= 0.0f && z_weight < __builtin_inff())) return fail(FP8_ERR_INVALID_ARG, "%s: z_weight is negative or not finite", who);
+    o.labels = labels; o.first = first; o.z_weight = z_weight;
     return FP8_OK;
 }
 
@@ -89,7 +103,7 @@ int fp8_gemm_act(const uint8_t* A, int fmtA, int transA, const uint8_t* B, int f
                  const void* residual, int residual_dtype, void* Z, int Z_dtype, const float* sD_dev, float* amax_out, int flags, void* stream)
 {
     const char* who = "fp8_gemm_act";
-    GemmArgs g; OpArgs o;
+    GemmArgs g; OpArgs o{};
     if (int e = fill_op(who, g, o, OP_ACT, A, fmtA, transA, B, fmtB, transB, D, out_kind, M, N, K, sA_dev, nsA, sB_dev, nsB, act, sD_dev, amax_out, flags, stream)) return e;
     if (int e = check_side(who, "bias", bias, bias_dtype, false)) return e;
     if (int e = check_side(who, "residual", residual, residual_dtype, false)) return e;
@@ -115,7 +129,7 @@ int fp8_gemm_act_grad(const uint8_t* A, int fmtA, int transA, const uint8_t* B, 
                       void* workspace, size_t workspace_bytes, const float* sD_dev, float* amax_out, int flags, void* stream)
 {
     const char* who = "fp8_gemm_act_grad";
-    GemmArgs g; OpArgs o;
+    GemmArgs g; OpArgs o{};
     if (int e = fill_op(who, g, o, OP_ACT_GRAD, A, fmtA, transA, B, fmtB, transB, D, out_kind, M, N, K, sA_dev, nsA, sB_dev, nsB, act, sD_dev, amax_out, flags, stream)) return e;
     if (int e = check_side(who, "Z", Z, Z_dtype, M > 0 && N > 0)) return e;
     if (Z && overlap(D, bytes_of(M, N, out_elem_size(out_kind)), Z, bytes_of(M, N, out_elem_size(Z_dtype))) && (D != Z || out_kind != Z_dtype))
@@ -136,7 +150,7 @@ int fp8_gemm_gated(const uint8_t* A, int fmtA, int transA, const uint8_t* B, int
                    const float* sH_dev, float* amax_out, int flags, void* stream)
 {
     const char* who = "fp8_gemm_gated";
-    GemmArgs g; OpArgs o;
+    GemmArgs g; OpArgs o{};
     if (int e = fill_op(who, g, o, OP_GATED, A, fmtA, transA, B, fmtB, transB, H, out_kind, M, F, K, sA_dev, nsA, sB_dev, nsB, act, sH_dev, amax_out, flags, stream)) return e;
     if (int e = check_side(who, "GU", GU, GU_dtype, false)) return e;
     const int64_t gu_bytes = bytes_of(M, 2 * F, out_elem_size(GU_dtype));
@@ -151,7 +165,7 @@ int fp8_gemm_gated_grad(const uint8_t* A, int fmtA, int transA, const uint8_t* B
                         const float* sD_dev, float* amax_out, int flags, void* stream)
 {
     const char* who = "fp8_gemm_gated_grad";
-    GemmArgs g; OpArgs o;
+    GemmArgs g; OpArgs o{};
     if (int e = fill_op(who, g, o, OP_GATED_GRAD, A, fmtA, transA, B, fmtB, transB, dGU, out_kind, M, F, K, sA_dev, nsA, sB_dev, nsB, act, sD_dev, amax_out, flags, stream)) return e;
     if (int e = check_side(who, "GU", GU, GU_dtype, M > 0 && F > 0)) return e;
     if (GU && overlap(dGU, bytes_of(M, 2 * F, out_elem_size(out_kind)), GU, bytes_of(M, 2 * F, out_elem_size(GU_dtype))) && (dGU != GU || out_kind != GU_dtype))
@@ -186,6 +200,111 @@ int fp8_grad_clip(int count, const void* const* x, const size_t* n, const int* d
             if (out[i] != x[i] && overlap(out[i], bytes, x[i], bytes)) return fail(FP8_ERR_INVALID_ARG, "%s: out[%d] overlaps x[%d] in part", who, i, i);
         }
     return launch_grad_clip(count, x, n, dtype, out ? out : (void* const*)x, norm, max_norm, (hipStream_t)stream);
+}
+
+size_t fp8_gemm_xent_workspace_size(int64_t M, int64_t N)
+{
+    if (M <= 0 || N < 0) return 0;
+    const size_t rows = (size_t)N / 32 + (N % 32 != 0) + 1;
+    return rows > SIZE_MAX / 8 / (size_t)M ? SIZE_MAX : rows * (size_t)M * 8;
+}
+
+int fp8_gemm_xent(const uint8_t* A, int fmtA, int transA, const uint8_t* B, int fmtB, int transB, int64_t M, int64_t N, int64_t K,
+                  const float* sA_dev, int64_t nsA, const float* sB_dev, int64_t nsB, const int64_t* labels, int64_t first, float z_weight,
+                  float* loss, float* lse, void* workspace, size_t workspace_bytes, int flags, void* stream)
+{
+    const char* who = "fp8_gemm_xent";
+    GemmArgs g; LossArgs o{};
+    // (no output of the product: the place of one that passes the checks)
+    if (int e = fill_op(who, g, o, OP_LOSS, A, fmtA, transA, B, fmtB, transB, lse, FP8_OUT_F32, M, N, K, sA_dev, nsA, sB_dev, nsB, FP8_ACT_NONE, nullptr, nullptr, flags, stream)) return e;
+    if (int e = fill_loss(who, o, M, labels, first, z_weight)) return e;
+    if (M == 0) return FP8_OK;
+    if (!loss || !lse || ((uintptr_t)loss | (uintptr_t)lse) % 4) return fail(FP8_ERR_INVALID_ARG, "%s: loss or lse is NULL or misaligned", who);
+    const size_t need = fp8_gemm_xent_workspace_size(M, N);
+    if (!workspace || (uintptr_t)workspace % 8 || workspace_bytes < need)
+        return fail(FP8_ERR_INVALID_ARG, "%s: the workspace is NULL, misaligned or smaller than %zu bytes", who, need);
+    const int64_t cells = 4 * M;
+    if (overlap(loss, cells, lse, cells) || overlap(loss, cells, workspace, (int64_t)need) || overlap(lse, cells, workspace, (int64_t)need) ||
+        overlap(labels, 8 * M, loss, cells) || overlap(labels, 8 * M, lse, cells) || overlap(labels, 8 * M, workspace, (int64_t)need))
+        return fail(FP8_ERR_INVALID_ARG, "%s: loss, lse, the workspace and labels overlap", who);
+    o.partials = workspace;
+    return launch_gemm_loss(g, o, loss, lse);
+}
+
+int fp8_gemm_xent_grad(const uint8_t* A, int fmtA, int transA, const uint8_t* B, int fmtB, int transB, void* D, int out_kind, int64_t M, int64_t N, int64_t K,
+                       const float* sA_dev, int64_t nsA, const float* sB_dev, int64_t nsB, const int64_t* labels, int64_t first, float z_weight,
+                       const float* lse, const float* dloss, int64_t ndloss, const float* sD_dev, float* amax_out, int flags, void* stream)
+{
+    const char* who = "fp8_gemm_xent_grad";
+    GemmArgs g; LossArgs o{};
+    if (int e = fill_op(who, g, o, OP_LOSS_GRAD, A, fmtA, transA, B, fmtB, transB, D, out_kind, M, N, K, sA_dev, nsA, sB_dev, nsB, FP8_ACT_NONE, sD_dev, amax_out, flags, stream)) return e;
+    if (int e = fill_loss(who, o, M, labels, first, z_weight)) return e;
+    if (ndloss != 1 && ndloss != M) return fail(FP8_ERR_INVALID_ARG, "%s: ndloss = %lld is neither 1 nor M", who, (long long)ndloss);
+    if (M > 0 && (!lse || !dloss || ((uintptr_t)lse | (uintptr_t)dloss) % 4)) return fail(FP8_ERR_INVALID_ARG, "%s: lse or dloss is NULL or misaligned", who);
+    const int64_t d_bytes = bytes_of(M, N, out_elem_size(out_kind));
+    if (overlap(D, d_bytes, labels, 8 * M) || overlap(D, d_bytes, lse, 4 * M) || overlap(D, d_bytes, dloss, 4 * ndloss) || overlap(D, d_bytes, A, bytes_of(M, K, 1)) ||
+        overlap(D, d_bytes, B, bytes_of(K, N, 1)))
+        return fail(FP8_ERR_INVALID_ARG, "%s: D overlaps another argument", who);
+    o.lse = lse; o.dloss = dloss; o.dloss_per_row = ndloss == M && M != 1;
+    return launch_gemm_loss(g, o, nullptr, nullptr);
+}
+
+int fp8_adamw(int count, void* const* p, const int* p_dtype, const void* const* g, const int* g_dtype, const size_t* n, void* const* m, void* const* v,
+              int state_kind, float* const* m_scale, float* const* v_scale, uint64_t seed, const float* weight_decay, const float* lr, const int64_t* step,
+              double beta1, double beta2, float eps, const float* norm, float max_norm, uint8_t* const* q, int q_fmt, const float* q_scale, float* q_amax,
+              int flags, void* stream)
+{
+    const char* who = "fp8_adamw";
+    clear_error();
+    if (flags & ~FP8_ADAMW_SKIP_NONFINITE) return fail(FP8_ERR_INVALID_ARG, "%s: unknown flag bits 0x%x", who, flags & ~FP8_ADAMW_SKIP_NONFINITE);
+    if (state_kind != FP8_STATE_F32 && state_kind != FP8_STATE_FP8) return fail(FP8_ERR_INVALID_ARG, "%s: state_kind %d is not an fp8_state_t", who, state_kind);
+    const bool states8 = state_kind == FP8_STATE_FP8;
+    if (int e = check_tensors(who, count, (const void* const*)p, n, p_dtype)) return e;
+    if (int e = check_tensors(who, count, g, n, g_dtype)) return e;
+    if (count > 0 && (!m || !v || (states8 && (!m_scale || !v_scale)))) return fail(FP8_ERR_INVALID_ARG, "%s: a list of states is NULL", who);
+    if (!lr || (uintptr_t)lr % 4 || !step || (uintptr_t)step % 8) return fail(FP8_ERR_INVALID_ARG, "%s: lr or step is NULL or misaligned", who);
+    if (!(beta1 >= 0.0 && beta1 < 1.0 && beta2 >= 0.0 && beta2 < 1.0)) return fail(FP8_ERR_INVALID_ARG, "%s: beta1 or beta2 lies outside [0, 1)", who);
+    if (!(eps >= 0.0f && eps < __builtin_inff())) return fail(FP8_ERR_INVALID_ARG, "%s: eps is negative or not finite", who);
+    if ((uintptr_t)norm % 4) return fail(FP8_ERR_INVALID_ARG, "%s: norm is misaligned", who);
+    if (norm && !(max_norm >= 0.0f)) return fail(FP8_ERR_INVALID_ARG, "%s: max_norm is negative or NaN", who);
+    if (q && !valid_format(q_fmt)) return fail(FP8_ERR_INVALID_ARG, "%s: q_fmt %d is not an fp8_format_t", who, q_fmt);
+    if (q && count > 0 && !q_scale) return fail(FP8_ERR_INVALID_ARG, "%s: q_scale is NULL", who);
+    if (((uintptr_t)q_scale | (uintptr_t)q_amax) % 4) return fail(FP8_ERR_INVALID_ARG, "%s: q_scale or q_amax is misaligned", who);
+    for (int i = 0; i < count; ++i) {
+        if (weight_decay && !(weight_decay[i] >= 0.0f && weight_decay[i] < __builtin_inff()))
+            return fail(FP8_ERR_INVALID_ARG, "%s: weight_decay[%d] is negative or not finite", who, i);
+        if (n[i] == 0) continue;
+        const int state = states8 ? 1 : 4;
+        if (!m[i] || !v[i] || (uintptr_t)m[i] % state || (uintptr_t)v[i] % state) return fail(FP8_ERR_INVALID_ARG, "%s: m[%d] or v[%d] is NULL or misaligned", who, i, i);
+        if (states8 && (!m_scale[i] || !v_scale[i] || ((uintptr_t)m_scale[i] | (uintptr_t)v_scale[i]) % 4))
+            return fail(FP8_ERR_INVALID_ARG, "%s: m_scale[%d] or v_scale[%d] is NULL or misaligned", who, i, i);
+        // (what one tensor's update reads and writes)
+        const int64_t k = (int64_t)n[i], blocks = 4 * ((k + FP8_STATE_BLOCK - 1) / FP8_STATE_BLOCK);
+        const struct { const void* p; int64_t bytes; } of[] = {{p[i], k * (p_dtype[i] == FP8_F32 ? 4 : 2)}, {g[i], k * (g_dtype[i] == FP8_F32 ? 4 : 2)}, {m[i], k * state}, {v[i], k * state},
+                                                               {q ? q[i] : nullptr, k}, {states8 ? m_scale[i] : nullptr, blocks}, {states8 ? v_scale[i] : nullptr, blocks}};
+        for (size_t a = 0; a < sizeof of / sizeof *of; ++a)
+            for (size_t b = 0; b < a; ++b)
+                if (overlap(of[a].p, of[a].bytes, of[b].p, of[b].bytes)) return fail(FP8_ERR_INVALID_ARG, "%s: arguments of tensor %d overlap", who, i);
+    }
+    // A weight that is in the list twice (tied weights) would be updated by two workgroups at once.
+    std::vector<std::pair<uintptr_t, uintptr_t>> taken;
+    try {
+        for (int i = 0; i < count; ++i)
+            if (n[i]) taken.emplace_back((uintptr_t)p[i], (uintptr_t)p[i] + n[i] * (p_dtype[i] == FP8_F32 ? 4 : 2));
+        std::sort(taken.begin(), taken.end());
+    } catch (const std::exception&) {
+        return fail(FP8_ERR_UNSUPPORTED, "%s: no host memory for a list of %d tensors", who, count);
+    }
+    for (size_t i = 1; i < taken.size(); ++i)
+        if (taken[i].first < taken[i - 1].second) return fail(FP8_ERR_INVALID_ARG, "%s: two of the weights share memory", who);
+    AdamwArgs a{};
+    a.count = count; a.p = p; a.p_dtype = p_dtype; a.g = g; a.g_dtype = g_dtype; a.n = n; a.m = m; a.v = v;
+    a.states8 = states8; a.m_scale = m_scale; a.v_scale = v_scale; a.seed = seed;
+    a.weight_decay = weight_decay; a.lr = lr; a.step = step; a.beta1 = beta1; a.beta2 = beta2; a.eps = eps;
+    a.norm = norm; a.max_norm = max_norm; a.q = q; a.q_fmt = q_fmt; a.q_scale = q_scale; a.q_amax = q_amax;
+    a.skip_nonfinite = (flags & FP8_ADAMW_SKIP_NONFINITE) != 0;
+    a.stream = (hipStream_t)stream;
+    return launch_adamw(a);
 }
 
 }  // extern "C"

@@ -82,4 +82,25 @@ int launch_grad_norm(int count, const void* const* x, const size_t* n, const int
 int launch_grad_clip(int count, const void* const* x, const size_t* n, const int* dtype, void* const* out, const float* norm, float max_norm,
                      hipStream_t stream);
 
+// Arguments of fp8_adamw, host arrays of `count` entries; m_scale, v_scale: of states in FP8; q: null, or entries that may be null.
+struct AdamwArgs {
+    int count;
+    void* const* p; const int* p_dtype;
+    const void* const* g; const int* g_dtype;
+    const size_t* n;
+    void* const* m; void* const* v;
+    bool states8;
+    float* const* m_scale; float* const* v_scale;
+    uint64_t seed;
+    const float* weight_decay;
+    const float* lr; const int64_t* step;
+    double beta1, beta2;
+    float eps;
+    const float* norm; float max_norm;
+    uint8_t* const* q; int q_fmt; const float* q_scale; float* q_amax;
+    int skip_nonfinite;
+    hipStream_t stream;
+};
+int launch_adamw(const AdamwArgs& a);
+
 }  // namespace fp8mm

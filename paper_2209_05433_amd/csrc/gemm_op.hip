@@ -1,6 +1,6 @@
 // Products with an operator behind them (gemm_op.hpp): which kernel takes a call, the kernel of plain FMAs that takes any, and the sum
 // of the partial column sums (gfx950).
-#include "gemm_op.hpp"
+#include "gemm_loss.hpp"
 
 #include <algorithm>
 
@@ -14,9 +14,10 @@ namespace {
 // ------------------------------------------------------------------------------------------
 constexpr int GT = 64, GK = 16;
 
-template <int FMT_A, int FMT_B, bool PAIR>
+// LOSS: the loss (o.op OP_LOSS) or its gradient.
+template <int FMT_A, int FMT_B, bool PAIR, bool LOSS = false>
 __global__ __launch_bounds__(256) void gemm_op_generic_kernel(const uint8_t* __restrict__ A, const uint8_t* __restrict__ B, void* D,
-                                                              int64_t M, int64_t N, int64_t K, OpArgs o, bool transA, bool transB)
+                                                              int64_t M, int64_t N, int64_t K, typename ArgsOf<LOSS>::type o, bool transA, bool transB)
 {
     constexpr int P = PAIR ? 2 : 1;
     __shared__ float As[GK][GT + 1];
@@ -55,7 +56,25 @@ __global__ __launch_bounds__(256) void gemm_op_generic_kernel(const uint8_t* __r
     const int left = col < N ? (int)(N - col < 4 ? N - col : 4) : 0;
     unsigned top = 0;
     float total[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (left > 0) {
+    if constexpr (LOSS) {
+        // (all lanes come along: 16 neighbouring ones hold a row)
+        const bool forward = o.op == OP_LOSS;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t row = m0 + ty * 4 + i, at = row < M ? row : M - 1;
+            const double a = 1.0 / (double)o.sA_dev[o.a_per_row ? at : 0];
+            float z[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) z[j] = acc[0][i][j] * (float)(a * op_column_factor(o, N, j < left ? col + j : N - 1, false));
+            if (forward) {
+                loss_logits<4>(o, M, N, row, col, left, label_column(o, at), z);
+                const LossPair pair = loss_pair<4, 16>(z);
+                if (row < M && tx == 0) ((LossPair*)o.partials)[(blockIdx.x % tiles_n) * M + row] = pair;
+            } else if (row < M && left > 0) {
+                top = max(top, loss_grad_row<4>(o, D, N, row, col, left, z, sD));
+            }
+        }
+    } else if (left > 0) {
         float bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         if (o.bias) load_row<4>(o.bias, o.bias_dtype, col, left, bias);
         double fy[4], fu[4];
@@ -81,7 +100,7 @@ __global__ __launch_bounds__(256) void gemm_op_generic_kernel(const uint8_t* __r
             for (int j = 0; j < 4; ++j) total[j] += y[j];
         }
     }
-    if (o.sums) {
+    if (!LOSS && o.sums) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) sums[ty][tx * 4 + j] = total[j];
         __syncthreads();
@@ -102,13 +121,19 @@ __global__ __launch_bounds__(256) void gemm_op_generic_kernel(const uint8_t* __r
 }
 
 template <int FA, int FB>
+void enqueue_generic(const GemmArgs& g, const LossArgs& o, unsigned tiles)
+{
+    enqueue(gemm_op_generic_kernel<FA, FB, false, true>, dim3(tiles), dim3(256), 0, g.stream, g.A, g.B, g.C, g.M, g.N, g.K, o, g.transA, g.transB);
+}
+template <int FA, int FB>
 void enqueue_generic(const GemmArgs& g, const OpArgs& o, unsigned tiles)
 {
     if (op_pair_in(o.op)) enqueue(gemm_op_generic_kernel<FA, FB, true>, dim3(tiles), dim3(256), 0, g.stream, g.A, g.B, g.C, g.M, g.N, g.K, o, g.transA, g.transB);
     else enqueue(gemm_op_generic_kernel<FA, FB, false>, dim3(tiles), dim3(256), 0, g.stream, g.A, g.B, g.C, g.M, g.N, g.K, o, g.transA, g.transB);
 }
 
-int launch_generic(const GemmArgs& g, const OpArgs& o)
+template <class ARGS>
+int launch_generic(const GemmArgs& g, const ARGS& o)
 {
     const int64_t tiles = ((g.M + GT - 1) / GT) * ((g.N + GT - 1) / GT);
     if (tiles > 0x7fffffffll) return fail(FP8_ERR_UNSUPPORTED, "gemm with an operator: %lld tiles of 64 x 64 exceed the grid limit", (long long)tiles);
@@ -162,23 +187,26 @@ OpPlan plan_op(const GemmArgs& g, const OpArgs& o)
     p.ep = o;
     p.ep.b_per_col = o.b_factors != B_ONE;
     if (g.K == 0 || (pair && !g.transB && g.N < 16)) return plain_fmas;
-    const bool chosen = !knob(FP8_KNOB_SMALL) && !knob(FP8_KNOB_GEMM_KERNEL) && !knob(FP8_KNOB_TILE_N);      // no knob asks for another kernel
+    const bool loss = o.op >= OP_LOSS;
+    const bool chosen = !loss && !knob(FP8_KNOB_SMALL) && !knob(FP8_KNOB_GEMM_KERNEL) && !knob(FP8_KNOB_TILE_N);      // no knob asks for another kernel
     if (chosen && op_skinny_takes(g, pair)) return {false, false, SMALL_NONE, (int)ACC_F16, 0, 0, true};
     const GemmPlan plan = plan_gemm(p, false);
     if (plan.kernel == GEMM_GENERIC) return plain_fmas;
     // Shapes and alignments outside the tiled kernel's, and any K that is no multiple of 16, are computed on the fp16 instructions, whatever the flag
     // says: callers are promised fp8_gemm's bound there.  (Of a gated block F is what has to be a multiple of 16, not 2 F.)
     const bool halves = !pair || g.transB || g.N % 16 == 0;
-    const int acc = plan.kernel == GEMM_MFMA_ANY || !halves || g.K % 16 ? (int)ACC_F16 : g.acc;
-    if (plan.small != SMALL_NONE) return {false, false, plan.small, acc, 0, 0, false};
+    // The loss exists in all its forms for E4M3 only; other formats go to tiles of 64 x 64 and the fp16 instructions.
+    const bool wide_formats = loss && (g.fmtA != FP8_E4M3 || g.fmtB != FP8_E4M3);
+    const int acc = plan.kernel == GEMM_MFMA_ANY || !halves || g.K % 16 || wide_formats ? (int)ACC_F16 : g.acc;
+    if (plan.small != SMALL_NONE && !wide_formats) return {false, false, plan.small, acc, 0, 0, false};
     // The tiled kernel exists for a weight in E4M3 (the format of weights); E5M2, and shapes and alignments that it does not take, go to tiles of 64 x 64 (4096 x 6144 x
     // 2048 with GELU 108 us, in E5M2 171; with K = 2047 226; up to some hundreds of tiles as fast as the plain product).
-    const bool tiled = plan.kernel != GEMM_MFMA_ANY && g.fmtB == FP8_E4M3 && halves && (!pair || !g.transB || (uint64_t)(g.N + TILE_M) * (uint64_t)g.K < (1ull << 32));
+    const bool tiled = plan.kernel != GEMM_MFMA_ANY && g.fmtB == FP8_E4M3 && halves && !(loss && (g.transA || wide_formats)) && (!pair || !g.transB || (uint64_t)(g.N + TILE_M) * (uint64_t)g.K < (1ull << 32));
     if (!tiled) return ((g.M + 63) / 64) * ((p.N + 63) / 64) > 0x7fffffffll ? plain_fmas : OpPlan{false, false, SMALL_64x64, acc, 0, 0, false};
     // The width whose rounds of 256 workgroups take less time, or both widths in one launch, by the plain product's model of run times with the
     // operator's own time on top (us of a 256-wide tile: fitted to 8192 x 8192 outputs over K = 256; it is the same per output in both widths).
     const TileTimes t = tile_times(acc, 2.0 * (double)((g.K + 2 * TILE_K - 1) / (2 * TILE_K)));
-    const double own = o.op == OP_GATED_GRAD ? 25.0 : o.op == OP_GATED ? 3.0 : o.op == OP_ACT_GRAD || o.side ? 12.0 : 7.0;
+    const double own = loss ? 7.0 : o.op == OP_GATED_GRAD ? 25.0 : o.op == OP_GATED ? 3.0 : o.op == OP_ACT_GRAD || o.side ? 12.0 : 7.0;
     const double wide = t.wide + own, narrow = t.narrow + 0.5 * own;
     const int64_t tiles_m = (g.M + TILE_M - 1) / TILE_M, wide_all = (p.N + 255) / 256, narrow_all = (p.N + 127) / 128;
     const double us_wide = tiles_makespan(tiles_m * wide_all, 0, wide, narrow), us_narrow = tiles_makespan(0, tiles_m * narrow_all, wide, narrow);
@@ -259,6 +287,33 @@ int launch_gemm_op(const GemmArgs& g, const OpArgs& args, float* dbias)
         return check_launch("gemm with an operator (column sums)");
     }
     return FP8_OK;
+}
+
+int launch_loss_join(const LossArgs& o, int64_t blocks, int64_t M, int64_t N, float* loss, float* lse, hipStream_t stream);      // (gemm_loss.hip)
+
+int launch_gemm_loss(const GemmArgs& g, const LossArgs& args, float* loss, float* lse)
+{
+    typedef int (*small_fn)(const GemmArgs&, const LossArgs&, int);
+    static const small_fn small[4] = {launch_loss_small_l0, launch_loss_small_l1, launch_loss_small_l2, launch_loss_small_l3};
+    typedef int (*tiled_fn)(const GemmArgs&, const LossArgs&);
+    static const tiled_fn tiled[2][2] = {{launch_loss_tiled_l0_a0, launch_loss_tiled_l0_a1}, {launch_loss_tiled_l1_a0, launch_loss_tiled_l1_a1}};
+    LossArgs o = args;
+    int64_t blocks = 0;                                      // of columns, with a pair each for every row
+    if (o.amax_out) {                                        // written, not accumulated
+        enqueue(op_zero_cell_kernel, dim3(1), dim3(1), 0, g.stream, (unsigned*)o.amax_out);
+        if (int e = check_launch("gradient of the loss (amax init)")) return e;
+    }
+    if (g.M > 0 && g.N > 0) {
+        const OpPlan plan = plan_op(g, o);
+        GemmArgs p = g;
+        p.acc = plan.acc; p.tile_n = plan.tile_n; p.wide_cols = o.wide_cols = plan.wide_cols;
+        // (a wave of the tiled kernel has half a tile's columns)
+        const int64_t width = plan.tiled ? plan.tile_n / 2 : plan.small == SMALL_32x32 ? 32 : 64;
+        blocks = plan.wide_cols ? 2 * (int64_t)plan.wide_cols + (g.N - 256 * (int64_t)plan.wide_cols + 63) / 64 : (g.N + width - 1) / width;
+        if (int e = plan.generic ? launch_generic(g, o) : plan.tiled ? tiled[g.transB][plan.acc == ACC_FP8 ? 1 : 0](p, o)
+                                                                     : small[(g.transA ? 2 : 0) + (g.transB ? 1 : 0)](p, o, plan.small)) return e;
+    }
+    return o.op == OP_LOSS && g.M > 0 ? launch_loss_join(o, blocks, g.M, g.N, loss, lse, g.stream) : (int)FP8_OK;
 }
 
 }  // namespace fp8mm

@@ -18,7 +18,7 @@
 
 namespace fp8mm {
 
-enum { OP_ACT = 0, OP_ACT_GRAD = 1, OP_GATED = 2, OP_GATED_GRAD = 3 };
+enum { OP_ACT = 0, OP_ACT_GRAD = 1, OP_GATED = 2, OP_GATED_GRAD = 3, OP_LOSS = 4, OP_LOSS_GRAD = 5 };      // (the last two: gemm_loss.hpp)
 // Factors of B: one; one of the gate's and one of the other projection's columns; one per column (2 N of them for OP_GATED).
 enum { B_ONE = 0, B_PAIR = 1, B_COLUMN = 2 };
 

@@ -7,9 +7,11 @@
 // other 32 the second projection's of the same 32 outputs: a thread adds up both before it combines them, and no sum goes through memory.
 // Column sums (the bias gradient) are added over the tile's rows in a fixed order and leave as one row of partial sums per row of tiles.
 //
-// This file is compiled once per pair of storage orders: -DFP8MM_LAYOUT.
+// The loss over a vocabulary (gemm_loss.hpp): 32 columns of a row are in eight neighbouring lanes; its pair over the tile's columns goes to memory.
+//
+// This file is compiled once per pair of storage orders, -DFP8MM_LAYOUT, and again with -DFP8MM_LOSS for the loss and its gradient.
 #include "gemm_small_tile.hpp"
-#include "gemm_op.hpp"
+#include "gemm_loss.hpp"
 
 #include <atomic>
 #include <type_traits>
@@ -68,11 +70,13 @@ struct PairOperand : Operand<KC, 2, S> {
     }
 };
 
-// Tile of 32 RM rows and 32 RN columns of op(B), NW waves, D chunks in flight per wave.  PAIR: the gated block (RN = 2).
-template <int FMT_A, int FMT_B, int ACC, bool A_KC, bool B_KC, int RM, int RN, int S, int NW, int D, bool PAIR>
+// Tile of 32 RM rows and 32 RN columns of op(B), NW waves, D chunks in flight per wave.  KIND: 0 one column of op(B) for each output, 1 the gated
+// block (RN = 2), 2 the loss, 3 its gradient.
+template <int FMT_A, int FMT_B, int ACC, bool A_KC, bool B_KC, int RM, int RN, int S, int NW, int D, int KIND>
 __global__ __launch_bounds__(64 * NW) void gemm_op_small_kernel(const uint8_t* __restrict__ A, const uint8_t* __restrict__ B, void* C,
-                                                                int64_t M, int64_t N, int64_t K, OpArgs o)
+                                                                int64_t M, int64_t N, int64_t K, typename ArgsOf<(KIND >= 2)>::type o)
 {
+    constexpr bool PAIR = KIND == 1;
     typedef Operand<A_KC, RM, S> OpA;
     typedef typename std::conditional<PAIR, PairOperand<B_KC, S>, Operand<B_KC, RN, S>>::type OpB;
     constexpr int CK = S * SK, WIDTH = 32 * RN / (PAIR ? 2 : 1);          // output columns of the tile
@@ -191,6 +195,13 @@ __global__ __launch_bounds__(64 * NW) void gemm_op_small_kernel(const uint8_t* _
     constexpr int TRIPS = (32 * RM * 8 + 64 * NW - 1) / (64 * NW);       // rows that a thread takes four columns of
     float first[PAIR ? TRIPS : 1][4];
     float column[RN][4];                                  // sums over the thread's rows
+    float logits[KIND == 2 ? TRIPS : 1][4 * RN];          // of the thread's rows, in base 2
+    if (KIND == 2) {
+#pragma unroll
+        for (int trip = 0; trip < TRIPS; ++trip)
+#pragma unroll
+            for (int e = 0; e < 4 * RN; ++e) logits[KIND == 2 ? trip : 0][e] = -__builtin_inff();
+    }
     unsigned top = 0;
 #pragma unroll
     for (int i = 0; i < RN; ++i) {
@@ -241,12 +252,31 @@ __global__ __launch_bounds__(64 * NW) void gemm_op_small_kernel(const uint8_t* _
                 z[e] = PAIR ? y[e] : 0.0f;
                 if (PAIR) y[e] = first[PAIR ? trip : 0][e];
             }
-            top = max(top, op_row<4, PAIR>(o, C, N, gm, gn, left, y, z, bias, sD));
+            if constexpr (KIND == 2) {
+                loss_logits<4>(o, M, N, gm, gn, left, label_column(o, gm), y);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) logits[trip][4 * i + e] = y[e];
+                continue;
+            } else if constexpr (KIND == 3) {
+                top = max(top, loss_grad_row<4>(o, C, N, gm, gn, left, y, sD));
+                continue;
+            } else {
+                top = max(top, op_row<4, PAIR>(o, C, N, gm, gn, left, y, z, bias, sD));
+            }
 #pragma unroll
             for (int e = 0; e < 4; ++e) column[i][e] += y[e];
         }
     }
-    if (!PAIR && o.sums) {
+    if constexpr (KIND == 2) {
+#pragma unroll
+        for (int trip = 0; trip < TRIPS; ++trip) {
+            const int u = tid + trip * 64 * NW;
+            const int64_t gm = m0 + (u >> 3);
+            const LossPair pair = loss_pair<4 * RN, 8>(logits[trip]);
+            if (u < 32 * RM * 8 && gm < M && (u & 7) == 0) ((LossPair*)o.partials)[(p / tiles_m) * M + gm] = pair;
+        }
+    }
+    if (KIND == 0 && o.sums) {
         // over the wave's rows, then over the waves, in their order; behind the first wave's sums and the factors, which have been read
         float* cells = (float*)(lds + RED);
         __syncthreads();
@@ -278,12 +308,13 @@ __global__ __launch_bounds__(64 * NW) void gemm_op_small_kernel(const uint8_t* _
     }
 }
 
-template <int FA, int FB, int ACC, int RM, int RN, int S, int NW, int D, bool PAIR>
-int launch_form(const GemmArgs& g, const OpArgs& o)
+template <int FA, int FB, int ACC, int RM, int RN, int S, int NW, int D, int KIND>
+int launch_form(const GemmArgs& g, const typename ArgsOf<(KIND >= 2)>::type& o)
 {
+    constexpr bool PAIR = KIND == 1;
     constexpr bool A_KC = (FP8MM_LAYOUT & 2) == 0, B_KC = (FP8MM_LAYOUT & 1) != 0;
     constexpr int LDS = NW * small_lds_per_wave<A_KC, B_KC, RM, RN, S>(), WIDTH = 32 * RN / (PAIR ? 2 : 1);
-    auto kern = gemm_op_small_kernel<FA, FB, ACC, A_KC, B_KC, RM, RN, S, NW, D, PAIR>;
+    auto kern = gemm_op_small_kernel<FA, FB, ACC, A_KC, B_KC, RM, RN, S, NW, D, KIND>;
     if (LDS > 65536) {
         // more dynamic LDS than the default limit: raised once per device
         static std::atomic<unsigned long long> attr_set{0ull};
@@ -294,28 +325,41 @@ int launch_form(const GemmArgs& g, const OpArgs& o)
     return check_launch("gemm with an operator (small tiles)");
 }
 
-template <int FA, int FB, int ACC, bool PAIR>
-int launch_acc(const GemmArgs& g, const OpArgs& o, int form)
+template <int FA, int FB, int ACC, int KIND>
+int launch_acc(const GemmArgs& g, const typename ArgsOf<(KIND >= 2)>::type& o, int form)
 {
+    constexpr bool PAIR = KIND == 1;
     constexpr bool A_KC = (FP8MM_LAYOUT & 2) == 0, B_KC = (FP8MM_LAYOUT & 1) != 0;
     switch (form) {
         case SMALL_32x32:                                 // (the gated block: 32 outputs of a row are 64 columns of op(B))
-            return launch_form<FA, FB, ACC, 1, PAIR ? 2 : 1, 2, 8, PAIR ? 1 : 2, PAIR>(g, o);
-        case SMALL_32x64: return launch_form<FA, FB, ACC, 1, 2, 2, 4, 2, PAIR>(g, o);
+            return launch_form<FA, FB, ACC, 1, PAIR ? 2 : 1, 2, 8, PAIR ? 1 : 2, KIND>(g, o);
+        case SMALL_32x64: return launch_form<FA, FB, ACC, 1, 2, 2, 4, 2, KIND>(g, o);
     }
     if constexpr (A_KC && B_KC) {
-        if (form == SMALL_64x64_LINES8) return launch_form<FA, FB, ACC, 2, 2, 2, 8, 1, PAIR>(g, o);
-        if (form == SMALL_64x64_LINES4) return launch_form<FA, FB, ACC, 2, 2, 2, 4, 1, PAIR>(g, o);
+        if (form == SMALL_64x64_LINES8) return launch_form<FA, FB, ACC, 2, 2, 2, 8, 1, KIND>(g, o);
+        if (form == SMALL_64x64_LINES4) return launch_form<FA, FB, ACC, 2, 2, 2, 4, 1, KIND>(g, o);
     }
-    return launch_form<FA, FB, ACC, 2, 2, 1, 4, 1, PAIR>(g, o);
+    return launch_form<FA, FB, ACC, 2, 2, 1, 4, 1, KIND>(g, o);
 }
 
+#if defined(FP8MM_LOSS)
+template <int KIND>
+int launch_loss(const GemmArgs& g, const LossArgs& o, int form)
+{
+    if (g.fmtA == FP8_E4M3 && g.fmtB == FP8_E4M3) return g.acc == ACC_FP8 ? launch_acc<FP8_E4M3, FP8_E4M3, ACC_FP8, KIND>(g, o, form) : launch_acc<FP8_E4M3, FP8_E4M3, ACC_F16, KIND>(g, o, form);
+    if (g.fmtA == FP8_E4M3) return launch_form<FP8_E4M3, FP8_E5M2, ACC_F16, 2, 2, 1, 4, 1, KIND>(g, o);
+    if (g.fmtB == FP8_E4M3) return launch_form<FP8_E5M2, FP8_E4M3, ACC_F16, 2, 2, 1, 4, 1, KIND>(g, o);
+    return launch_form<FP8_E5M2, FP8_E5M2, ACC_F16, 2, 2, 1, 4, 1, KIND>(g, o);
+}
+#else
 template <int FA, int FB>
 int launch_formats(const GemmArgs& g, const OpArgs& o, int form)
 {
-    if (op_pair_in(o.op)) return g.acc == ACC_FP8 ? launch_acc<FA, FB, ACC_FP8, true>(g, o, form) : launch_acc<FA, FB, ACC_F16, true>(g, o, form);
-    return g.acc == ACC_FP8 ? launch_acc<FA, FB, ACC_FP8, false>(g, o, form) : launch_acc<FA, FB, ACC_F16, false>(g, o, form);
+    if (op_pair_in(o.op)) return g.acc == ACC_FP8 ? launch_acc<FA, FB, ACC_FP8, 1>(g, o, form) : launch_acc<FA, FB, ACC_F16, 1>(g, o, form);
+    return g.acc == ACC_FP8 ? launch_acc<FA, FB, ACC_FP8, 0>(g, o, form) : launch_acc<FA, FB, ACC_F16, 0>(g, o, form);
 }
+
+#endif
 
 }  // namespace
 
@@ -323,11 +367,17 @@ int launch_formats(const GemmArgs& g, const OpArgs& o, int form)
 #error "compile with -DFP8MM_LAYOUT=0..3 (2 * transA + transB)"
 #endif
 
+#if defined(FP8MM_LOSS)
+#define FP8MM_LOSS_SMALL_NAME_(l) launch_loss_small_l##l
+#define FP8MM_LOSS_SMALL_NAME(l) FP8MM_LOSS_SMALL_NAME_(l)
+int FP8MM_LOSS_SMALL_NAME(FP8MM_LAYOUT)(const GemmArgs& g, const LossArgs& o, int form) { return o.op == OP_LOSS ? launch_loss<2>(g, o, form) : launch_loss<3>(g, o, form); }
+#else
 int FP8MM_OP_SMALL_NAME(FP8MM_LAYOUT)(const GemmArgs& g, const OpArgs& o, int form)
 {
     if (g.fmtA == FP8_E4M3)
         return g.fmtB == FP8_E4M3 ? launch_formats<FP8_E4M3, FP8_E4M3>(g, o, form) : launch_formats<FP8_E4M3, FP8_E5M2>(g, o, form);
     return g.fmtB == FP8_E4M3 ? launch_formats<FP8_E5M2, FP8_E4M3>(g, o, form) : launch_formats<FP8_E5M2, FP8_E5M2>(g, o, form);
 }
+#endif
 
 }  // namespace fp8mm

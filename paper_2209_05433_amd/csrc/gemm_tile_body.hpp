@@ -48,6 +48,7 @@
 
 #include "gemm_epilogue.hpp"
 #include "gemm_op_epilogue.hpp"
+#include "gemm_loss_epilogue.hpp"
 #include "gemm_slabs.hpp"
 
 #include <type_traits>
@@ -217,7 +218,7 @@ template <> struct TileOutput<0> { typedef void* __restrict__ type; };
 // bf16 output with rows on 16-byte boundaries, no output maximum, no K slices.
 //
 // OP: 0 the plain product; 1 bias, activation and residual behind it, 2 the gated block, whose tile has BN / 2 output columns, 3 the gradients
-// (1 to 3: ep is an OpArgs, N counts output columns; no slices of K, not persistent).
+// of the feed-forward operators, 4 the loss over a vocabulary, 5 its gradient (1 to 3: ep is an OpArgs, 4 and 5: a LossArgs; N counts output columns; no slices of K, not persistent).
 //
 // The body works on tile number `bid_in` of a region of the output that starts at column n_begin and
 // is tiles_n tiles wide (the whole output for the plain kernel; see gemm_mixed_kernel).
@@ -703,7 +704,8 @@ __device__ __forceinline__ void gemm_tile_body(
     __builtin_amdgcn_s_waitcnt(0xC07F);
     __builtin_amdgcn_s_barrier();                           // every wave is done with the operand slabs
     if constexpr (OP == 1 || OP == 3) beside.touched();
-    if constexpr (OP != 0) op_store_tile<NB, OP>(acc, smem, static_cast<const OpArgs&>(ep), C, M, N, m0, n0, w);
+    if constexpr (OP >= 4) loss_store_tile<NB, OP>(acc, smem, static_cast<const LossArgs&>(ep), C, M, N, m0, n0, w);
+    else if constexpr (OP != 0) op_store_tile<NB, OP>(acc, smem, static_cast<const OpArgs&>(ep), C, M, N, m0, n0, w);
     else store_tile<NB, false>(acc, smem, ep, C, M, N, m0, n0, w);
 }
 

@@ -31,7 +31,7 @@ struct Failed {};                        // a Python exception is set
 }
 
 // The arguments of one call, by position or by name, in the order of `names`.
-constexpr int kMost = 18;
+constexpr int kMost = 21;
 struct Args {
     PyObject* v[kMost] = {};
     Args(const char* fn, const char* const* names, int count, int required, PyObject* const* args, Py_ssize_t nargs, PyObject* kw)
@@ -98,14 +98,15 @@ int truth(PyObject* o)
 }
 
 // float(o)
-float real(PyObject* o)
+double real64(PyObject* o)
 {
     PyObject* f = PyNumber_Float(o);
     if (!f) throw Failed{};
     const double d = PyFloat_AS_DOUBLE(f);
     Py_DECREF(f);
-    return (float)d;
+    return d;
 }
+float real(PyObject* o) { return (float)real64(o); }
 
 // None: torch's current stream; an object with a cuda_stream, or what int() makes the handle itself.
 void* stream_of(PyObject* o)
@@ -611,7 +612,11 @@ struct OpProduct {
     float* amax;
     int64_t M, N, K, nA, nB;
     int fa, fb, tA, tB, kind, act, flags;
-    OpProduct(const Args& a, bool pair_in, bool pair_out, int at_sD, const char* output, const char* shapes)
+    OpProduct(const Args& a, bool pair_in, bool pair_out, int at_sD, const char* output, const char* shapes) : OpProduct(a, at_sD, output, shapes, pair_in, pair_out)
+    {
+        act = small(a[10]);
+    }
+    OpProduct(const Args& a, int at_sD, const char* output, const char* shapes, bool pair_in = false, bool pair_out = false)
     {
         const at::Tensor &ta = tensor(a[0], "A"), &tb = tensor(a[3], "B"), &d = tensor(a[6], output), &fA = tensor(a[8], "sA"), &fB = tensor(a[9], "sB");
         tA = truth(a[2]); tB = truth(a[5]); kind = small_of_int(a[7]);
@@ -632,7 +637,7 @@ struct OpProduct {
         nA = fA.numel(); nB = fB.numel();
         sD = is_none(a[at_sD]) ? nullptr : cells(a[at_sD], "the output's factor", 1);
         amax = is_none(a[at_sD + 1]) ? nullptr : cells_out(a[at_sD + 1], "amax_out", 1);
-        fa = small(a[1]); fb = small(a[4]); act = small(a[10]); flags = small_of_int(a[at_sD + 2]);
+        fa = small(a[1]); fb = small(a[4]); act = FP8_ACT_NONE; flags = small_of_int(a[at_sD + 2]);
         stream = stream_of(a[at_sD + 3]);
     }
     // A tensor beside the product, of the given number of columns (rows < 0: a vector), or None.
@@ -753,6 +758,138 @@ ENTRY(fp8_grad_clip, 3, "xs", "norm", "max_norm", "outs", "stream")
     return checked([&] { return ::fp8_grad_clip((int)g.x.size(), g.x.data(), g.n.data(), g.dtype.data(), out.data(), norm, most, s); });
 }
 
+// ---- the two ends of a training step -----------------------------------------------------------------------
+// What the loss and its gradient have in common.  `at`: of the first of first, z_weight.
+struct LossInputs {
+    const int64_t* labels;
+    int64_t first;
+    float z_weight;
+    LossInputs(PyObject* o, PyObject* first_, PyObject* z, int64_t M)
+    {
+        const at::Tensor& y = tensor(o, "labels");
+        if (y.scalar_type() != at::kLong || y.numel() != M) {
+            PyErr_Format(PyExc_ValueError, "labels must be an int64 device tensor of %lld values", (long long)M);
+            throw Failed{};
+        }
+        labels = (const int64_t*)device_or_null(y, "labels");
+        first = first_ ? (int64_t)low_bits_of_int(first_) : 0;
+        z_weight = z ? real(z) : 0.0f;
+    }
+};
+float* cells_out_or_null(PyObject* o, const char* what, int64_t count) { return (float*)written_or_null(cells_tensor(o, what, count), what); }
+const float* cells_or_null(PyObject* o, const char* what, int64_t count) { return (const float*)device_or_null(cells_tensor(o, what, count), what); }
+
+ENTRY(fp8_gemm_xent, 12, "A", "fmtA", "transA", "B", "fmtB", "transB", "labels", "loss", "lse", "workspace", "sA", "sB", "first", "z_weight", "flags", "stream")
+{
+    const int tA = truth(a[2]), tB = truth(a[5]);
+    const at::Tensor &ta = tensor(a[0], "A"), &tb = tensor(a[3], "B"), &ws = tensor(a[9], "workspace"), &fA = tensor(a[10], "sA"), &fB = tensor(a[11], "sB");
+    if (ta.dim() != 2 || tb.dim() != 2 || !is_bytes(ta) || !is_bytes(tb)) raise(PyExc_ValueError, "%s", kBytes2d);
+    const int64_t M = ta.size(tA ? 1 : 0), K = ta.size(tA ? 0 : 1), N = tb.size(tB ? 0 : 1);
+    if (tb.size(tB ? 1 : 0) != K) raise(PyExc_ValueError, "shapes do not form op(A)[M,K] op(B)[K,N]");
+    if (fA.scalar_type() != at::kFloat || fB.scalar_type() != at::kFloat) raise(PyExc_ValueError, "sA and sB must be fp32 device tensors");
+    const LossInputs in(a[6], a[12], a[13], M);
+    float *loss = cells_out_or_null(a[7], "loss", M), *lse = cells_out_or_null(a[8], "lse", M);
+    const uint8_t *A = (const uint8_t*)device_or_null(ta, "A"), *B = (const uint8_t*)device_or_null(tb, "B");
+    const float *sA = (const float*)device(fA, "sA"), *sB = (const float*)device(fB, "sB");
+    const int64_t nA = fA.numel(), nB = fB.numel();
+    void* w = written_or_null(ws, "workspace");
+    const size_t bytes = (size_t)ws.numel() * ws.element_size();
+    const int fa = small(a[1]), fb = small(a[4]), flags = small_of_int(a[14]);
+    void* s = stream_of(a[15]);
+    return checked([&] { return ::fp8_gemm_xent(A, fa, tA, B, fb, tB, M, N, K, sA, nA, sB, nB, in.labels, in.first, in.z_weight, loss, lse, w, bytes, flags, s); });
+}
+
+ENTRY(fp8_gemm_xent_grad, 13, "A", "fmtA", "transA", "B", "fmtB", "transB", "D", "out_kind", "sA", "sB", "labels", "lse", "dloss", "first", "z_weight", "sD", "amax_out", "flags",
+      "stream")
+{
+    const OpProduct p(a, 15, "D", "shapes do not form D[M,N] = op(A)[M,K] op(B)[K,N]");
+    const LossInputs in(a[10], a[13], a[14], p.M);
+    const float* lse = cells_or_null(a[11], "lse", p.M);
+    const at::Tensor& d = cells_tensor(a[12], "dloss", -1);
+    const float* dloss = (const float*)device_or_null(d, "dloss");
+    const int64_t n = d.numel();
+    return checked([&] { return ::fp8_gemm_xent_grad(p.A, p.fa, p.tA, p.B, p.fb, p.tB, p.D, p.kind, p.M, p.N, p.K, p.sA, p.nA, p.sB, p.nB, in.labels, in.first, in.z_weight, lse, dloss, n,
+                                                     p.sD, p.amax, p.flags, p.stream); });
+}
+
+// A list of tensors beside another one's, of a type (undefined: the type of each is its own) and of as many elements, or as many blocks.
+template <class T>
+std::vector<T*> beside(PyObject* o, const std::vector<size_t>& n, size_t unit, at::ScalarType type, const char* what, bool gaps = false)
+{
+    const Sequence ts(o, "expected a sequence of tensors");
+    std::vector<T*> p;
+    p.reserve(n.size());
+    bool fine = (size_t)ts.size() == n.size();
+    for (size_t i = 0; fine && i < n.size(); ++i) {
+        if (gaps && is_none(ts[(Py_ssize_t)i])) { p.push_back(nullptr); continue; }
+        const at::Tensor& t = tensor(ts[(Py_ssize_t)i], what);
+        fine = t.scalar_type() == type && (size_t)t.numel() == (n[i] + unit - 1) / unit;
+        if (fine) p.push_back((T*)written_or_null(t, what));
+    }
+    if (!fine) raise(PyExc_ValueError, "%s must be one tensor for each parameter, of the type and size that belong to it", what);
+    return p;
+}
+
+ENTRY(fp8_adamw, 6, "params", "grads", "m", "v", "step", "lr", "beta1", "beta2", "eps", "weight_decay", "norm", "max_norm", "m_scale", "v_scale", "seed", "q", "q_scale", "q_amax", "q_fmt",
+      "flags", "stream")
+{
+    const Sequence ps(a[0], "params must be a sequence of tensors"), gs(a[1], "grads must be a sequence of tensors");
+    const Gradients g(gs);
+    const size_t count = (size_t)ps.size();
+    std::vector<void*> p;
+    std::vector<int> p_dtype;
+    if (g.n.size() != count) raise(PyExc_ValueError, "grads must be one tensor for each parameter");
+    for (size_t i = 0; i < count; ++i) {
+        const at::Tensor& t = tensor(ps[(Py_ssize_t)i], "parameter");
+        if ((size_t)t.numel() != g.n[i]) raise(PyExc_ValueError, "parameters and gradients must have as many elements");
+        p_dtype.push_back(dtype_of(t));
+        p.push_back(written_or_null(t, "parameter"));
+    }
+    const bool states8 = !is_none(a[12]);
+    if (states8 != !is_none(a[13])) raise(PyExc_ValueError, "m_scale and v_scale belong together");
+    const at::ScalarType state = states8 ? at::kByte : at::kFloat;
+    const std::vector<void*> m = beside<void>(a[2], g.n, 1, state, "m"), v = beside<void>(a[3], g.n, 1, state, "v");
+    std::vector<float*> ms, vs;
+    if (states8) {
+        ms = beside<float>(a[12], g.n, FP8_STATE_BLOCK, at::kFloat, "m_scale");
+        vs = beside<float>(a[13], g.n, FP8_STATE_BLOCK, at::kFloat, "v_scale");
+    }
+    const at::Tensor& t = tensor(a[4], "step");
+    if (t.scalar_type() != at::kLong || t.numel() != 1) raise(PyExc_ValueError, "step must be an int64 device tensor of one value");
+    const int64_t* step = (const int64_t*)device(t, "step");
+    const float* lr = cells(a[5], "lr", 1);
+    const double beta1 = a[6] ? real64(a[6]) : 0.9, beta2 = a[7] ? real64(a[7]) : 0.999;
+    const float eps = a[8] ? real(a[8]) : 1e-8f, most = a[11] ? real(a[11]) : HUGE_VALF;
+    std::vector<float> decay;
+    if (!is_none(a[9])) {
+        if (PyFloat_Check(a[9]) || PyLong_Check(a[9])) decay.assign(count, real(a[9]));
+        else {
+            const Sequence d(a[9], "weight_decay must be a number or a sequence of numbers");
+            for (Py_ssize_t i = 0; i < d.size(); ++i) decay.push_back(real(d[i]));
+            if (decay.size() != count) raise(PyExc_ValueError, "weight_decay must be a number, or one for each parameter");
+        }
+    }
+    const float* norm = is_none(a[10]) ? nullptr : cells(a[10], "norm", 1);
+    const uint64_t seed = a[14] ? low_bits_of_int(a[14]) : 0;
+    std::vector<uint8_t*> q;
+    const float* q_scale = nullptr;
+    float* q_amax = nullptr;
+    const bool copies = !is_none(a[15]);
+    if (copies) {
+        q = beside<uint8_t>(a[15], g.n, 1, at::kByte, "q", true);
+        if (is_none(a[16])) raise(PyExc_ValueError, "q needs q_scale");
+        q_scale = cells_or_null(a[16], "q_scale", (int64_t)count);
+    } else if (!is_none(a[16])) {
+        raise(PyExc_ValueError, "q_scale belongs to q");
+    }
+    if (!is_none(a[17])) q_amax = cells_out_or_null(a[17], "q_amax", (int64_t)count);
+    const int fmt = small_of_int(a[18]), flags = small_of_int(a[19]);
+    void* s = stream_of(a[20]);
+    return checked([&] { return ::fp8_adamw((int)count, p.data(), p_dtype.data(), g.x.data(), g.dtype.data(), g.n.data(), m.data(), v.data(), states8 ? FP8_STATE_FP8 : FP8_STATE_F32,
+                                            states8 ? ms.data() : nullptr, states8 ? vs.data() : nullptr, seed, decay.empty() ? nullptr : decay.data(), lr, step, beta1, beta2, eps,
+                                            norm, most, copies ? q.data() : nullptr, fmt, q_scale, q_amax, flags, s); });
+}
+
 // Called once by the package: the exception that failing calls raise.
 PyObject* py_set_error(PyObject*, PyObject* type)
 {
@@ -815,6 +952,16 @@ PyMethodDef methods[] = {
     METHOD(fp8_grad_norm, "fp8_grad_norm(xs, norm_out, workspace, stream=None)\n--\n\nnorm_out (one fp32 value) = the 2-norm over all tensors of xs (float32 or bfloat16, mixed); workspace: "
            "device tensor\nof at least FP8_GRAD_NORM_WORKSPACE_BYTES bytes, zero-filled once before its first use."),
     METHOD(fp8_grad_clip, "fp8_grad_clip(xs, norm, max_norm, outs=None, stream=None)\n--\n\nouts = xs * min(1, max_norm / (norm + 1e-6)), in place where outs is None."),
+    METHOD(fp8_gemm_xent, "fp8_gemm_xent(A, fmtA, transA, B, fmtB, transB, labels, loss, lse, workspace, sA, sB, first=0, z_weight=0.0, flags=0, stream=None)\n--\n\n"
+           "Cross entropy of the logits z = op(A) op(B) / (sA sB), M rows, N columns: lse = log sum exp(z), loss = lse - z[label - first] + z_weight lse^2\n"
+           "(M fp32 values each; labels: M int64 values, negative ones: loss 0); workspace (any dtype) of at least\nfp8_gemm_xent_workspace_size(M, N) bytes."),
+    METHOD(fp8_gemm_xent_grad, "fp8_gemm_xent_grad(A, fmtA, transA, B, fmtB, transB, D, out_kind, sA, sB, labels, lse, dloss, first=0, z_weight=0.0, sD=None, amax_out=None, flags=0, "
+           "stream=None)\n--\n\nD = dloss (exp(z - lse) (1 + 2 z_weight lse) - [the label's column]), z as in fp8_gemm_xent, lse as it left it; dloss: one or M\nfp32 values."),
+    METHOD(fp8_adamw, "fp8_adamw(params, grads, m, v, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=None, norm=None, max_norm=inf, m_scale=None, v_scale=None, seed=0, q=None, "
+           "q_scale=None, q_amax=None, q_fmt=FP8_E4M3, flags=0, stream=None)\n--\n\nOne step of AdamW in place on sequences of tensors; step (int64), lr (fp32): device tensors of one value; "
+           "weight_decay: a number or\none for each parameter; norm: None or what fp8_grad_norm wrote, for clipping to max_norm.  States m, v: float32, or uint8 with\n"
+           "m_scale, v_scale of one fp32 factor for each FP8_STATE_BLOCK elements.  q: None, or uint8 tensors (None: no copy) that receive the new\n"
+           "weights in FP8 with the factors q_scale (one for each parameter); q_amax: their largest magnitudes."),
     {"set_error", py_set_error, METH_O, "The exception class that failing calls raise."},
     {nullptr, nullptr, 0, nullptr}};
 
