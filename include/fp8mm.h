@@ -506,7 +506,7 @@ int fp8_grad_clip(int count, const void* const* x, const size_t* n, const int* d
  *   workspace  device, 8-byte aligned, at least fp8_gemm_xent_workspace_size(M, N) bytes = 8 M (ceil(N / 32) + 1) (SIZE_MAX, if a size_t holds no
  *              such number); contents on entry are irrelevant; calls that may overlap need workspaces of their own
  * z_ij meets the bound of fp8_gemm (fp8_gemm_mfma8 with FP8_GEMM_MFMA8).  Sums of exponentials are held in 32 bits around the row's maximum in each run of up to
- * 128 columns and joined in 64: beyond what the z_ij are off by, lse is within 2^-22 (|lse| + max |z|) + 2^-20.  Results are the same in every run.
+ * 128 columns and joined in 64: beyond what the z_ij are off by, lse is within 2^-22 (|lse| + max |z|) + 2^-19.  Results are the same in every run.
  * Logits of -infinity count nothing (all of them: lse = -infinity); +infinity makes lse +infinity, NaN makes it NaN.
  */
 size_t fp8_gemm_xent_workspace_size(int64_t M, int64_t N);

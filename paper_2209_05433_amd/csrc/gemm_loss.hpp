@@ -61,9 +61,11 @@ __device__ __forceinline__ LossPair loss_pair(const float (&t)[C])
     for (int d = FIRST; d < LANES * FIRST; d <<= 1) top = __builtin_fmaxf(top, __shfl_xor(top, d, 64));
     constexpr float most = 3.4028234663852886e38f;
     const float ref = __builtin_fminf(__builtin_fmaxf(top, -most), most);
-    float s = 0.0f;
+    // (four runs: fewer roundings behind one another)
+    float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int i = 0; i < C; ++i) s += __builtin_amdgcn_exp2f(t[i] - ref);
+    for (int i = 0; i < C; ++i) part[i % 4] += __builtin_amdgcn_exp2f(t[i] - ref);
+    float s = (part[0] + part[1]) + (part[2] + part[3]);
 #pragma unroll
     for (int d = FIRST; d < LANES * FIRST; d <<= 1) s += __shfl_xor(s, d, 64);
     return {ref, s};

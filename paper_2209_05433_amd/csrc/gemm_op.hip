@@ -136,7 +136,7 @@ template <class ARGS>
 int launch_generic(const GemmArgs& g, const ARGS& o)
 {
     const int64_t tiles = ((g.M + GT - 1) / GT) * ((g.N + GT - 1) / GT);
-    if (tiles > 0x7fffffffll) return fail(FP8_ERR_UNSUPPORTED, "gemm with an operator: %lld tiles of 64 x 64 exceed the grid limit", (long long)tiles);
+    if (tiles > (int64_t)UINT32_MAX / 256) return fail(FP8_ERR_UNSUPPORTED, "gemm with an operator: %lld tiles of 64 x 64 exceed the grid limit", (long long)tiles);
     if (g.fmtA == FP8_E4M3) {
         if (g.fmtB == FP8_E4M3) enqueue_generic<FP8_E4M3, FP8_E4M3>(g, o, (unsigned)tiles);
         else enqueue_generic<FP8_E4M3, FP8_E5M2>(g, o, (unsigned)tiles);

@@ -321,6 +321,7 @@ int launch_form(const GemmArgs& g, const typename ArgsOf<(KIND >= 2)>::type& o)
         if (int e = raise_lds_limit((const void*)kern, LDS, attr_set)) return e;
     }
     const int64_t tiles = ((g.M + 32 * RM - 1) / (32 * RM)) * ((g.N + WIDTH - 1) / WIDTH);
+    if (tiles > (int64_t)UINT32_MAX / (64 * NW)) return fail(FP8_ERR_UNSUPPORTED, "gemm with an operator: %lld tiles of %d threads exceed the grid limit", (long long)tiles, 64 * NW);
     enqueue(kern, dim3((unsigned)tiles), dim3(64 * NW), LDS, g.stream, g.A, g.B, g.C, g.M, g.N, g.K, o);
     return check_launch("gemm with an operator (small tiles)");
 }
