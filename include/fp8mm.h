@@ -541,8 +541,8 @@ int fp8_gemm_xent_grad(const uint8_t* A, int fmtA, int transA, const uint8_t* B,
  *   p, p_dtype  the weights, n[i] elements, fp8_dtype_t; g, g_dtype: their gradients
  *   state_kind  FP8_STATE_F32: m[i], v[i] are n[i] fp32 values.
  *               FP8_STATE_FP8: n[i] bytes of E4M3 each, of m and of sqrt(v), and m_scale[i], v_scale[i] ceil(n[i] / 128) fp32 factors, one for each 128 elements:
- *               m = decode(byte) / factor.  A state of zeros is bytes 0 and factors 1.  The step leaves factors of 448 over the block's largest magnitude (1 where
- *               that is 0 or not finite) and bytes rounded stochastically as by fp8_quantize_sr: to the neighbour above where T + r >= 2^16; r of m the low, of sqrt(v)
+ *               m = decode(byte) / factor.  A state of zeros is bytes 0 and factors 1.  The step leaves factors of 448 times the reciprocal of the block's largest magnitude
+ *               (1 where that is 0 or not finite) and bytes rounded stochastically as by fp8_quantize_sr: to the neighbour above where T + r >= 2^16; r of m the low, of sqrt(v)
  *               the high half of word e % 4 of Philox4x32-10 with the counter (e / 4: two words, t's low word, i) and the key `seed`, e: the element, i: the tensor.
  *               A positive sqrt(v) never becomes 0.  Factors that are not finite and > 0 are not a state.
  *   seed        of FP8 states; one for a whole run of training will do
