@@ -3,7 +3,7 @@ of bench.py) for gfx950 with hipcc, and the Python binding _native.so with g++, 
 
 Every translation unit is compiled to an object of its own, in parallel; the tiled GEMM source is
 compiled eight times, once per pair of operand storage orders (-DFP8MM_LAYOUT=0..3) and
-accumulation mode (-DFP8MM_ACC=0|1)."""
+accumulation mode (-DFP8MM_ACC=0|1); sources that the loss over a vocabulary has ends in once more for it (-DFP8MM_LOSS)."""
 from __future__ import annotations
 
 import os
@@ -30,6 +30,7 @@ UNITS = [("gemm_tiled.hip", ["-DFP8MM_LAYOUT=%d" % k, "-DFP8MM_ACC=%d" % a], "ge
         [("gemm_op_small.hip", ["-DFP8MM_LAYOUT=%d" % k], "gemm_op_small_l%d.o" % k) for k in range(4)] + \
         [("gemm_op_tiled.hip", ["-DFP8MM_LAYOUT=%d" % k, "-DFP8MM_ACC=%d" % a, "-DFP8MM_LOSS"], "gemm_loss_tiled_l%d_a%d.o" % (k, a))
          for k in range(2) for a in range(2)] + \
+        [("gemm_mfma_any.hip", ["-DFP8MM_LAYOUT=%d" % k, "-DFP8MM_LOSS"], "gemm_loss_any_l%d.o" % k) for k in range(4)] + \
         [("gemm_op_small.hip", ["-DFP8MM_LAYOUT=%d" % k, "-DFP8MM_LOSS"], "gemm_loss_small_l%d.o" % k) for k in range(4)] + \
         [("gemm_dispatch.hip", [], "gemm_dispatch.o"), ("gemm_splitk.hip", [], "gemm_splitk.o"),
          ("cast_kernels.hip", [], "cast_kernels.o"),

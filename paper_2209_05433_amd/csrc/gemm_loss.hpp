@@ -37,6 +37,11 @@ int launch_loss_tiled_l0_a0(const GemmArgs& g, const LossArgs& o);
 int launch_loss_tiled_l0_a1(const GemmArgs& g, const LossArgs& o);
 int launch_loss_tiled_l1_a0(const GemmArgs& g, const LossArgs& o);
 int launch_loss_tiled_l1_a1(const GemmArgs& g, const LossArgs& o);
+// The kernel for any shape (gemm_mfma_any.hip), both operands in E4M3; width: 256 or 128 columns a tile.
+int launch_loss_any_l0(const GemmArgs& g, const LossArgs& o, int width);
+int launch_loss_any_l1(const GemmArgs& g, const LossArgs& o, int width);
+int launch_loss_any_l2(const GemmArgs& g, const LossArgs& o, int width);
+int launch_loss_any_l3(const GemmArgs& g, const LossArgs& o, int width);
 int launch_loss_small_l0(const GemmArgs& g, const LossArgs& o, int form);
 int launch_loss_small_l1(const GemmArgs& g, const LossArgs& o, int form);
 int launch_loss_small_l2(const GemmArgs& g, const LossArgs& o, int form);
@@ -50,13 +55,14 @@ namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f;
 
-// The pair of a row of which a lane holds C values t (-infinity outside) and LANES neighbouring lanes the rest, in all of these lanes.
+// The pair of a row of which a lane holds C values x, t = g x (g > 0; outside: -infinity), and LANES lanes, FIRST apart, the rest; in all of these lanes.
 template <int C, int LANES, int FIRST = 1>
-__device__ __forceinline__ LossPair loss_pair(const float (&t)[C])
+__device__ __forceinline__ LossPair loss_pair(const float (&x)[C], float g = 1.0f)
 {
-    float top = t[0];
+    float top = x[0];
 #pragma unroll
-    for (int i = 1; i < C; ++i) top = __builtin_fmaxf(top, t[i]);
+    for (int i = 1; i < C; ++i) top = __builtin_fmaxf(top, x[i]);
+    top *= g;
 #pragma unroll
     for (int d = FIRST; d < LANES * FIRST; d <<= 1) top = __builtin_fmaxf(top, __shfl_xor(top, d, 64));
     constexpr float most = 3.4028234663852886e38f;
@@ -64,7 +70,7 @@ __device__ __forceinline__ LossPair loss_pair(const float (&t)[C])
     // (four runs: fewer roundings behind one another)
     float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int i = 0; i < C; ++i) part[i % 4] += __builtin_amdgcn_exp2f(t[i] - ref);
+    for (int i = 0; i < C; ++i) part[i % 4] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], g, -ref));
     float s = (part[0] + part[1]) + (part[2] + part[3]);
 #pragma unroll
     for (int d = FIRST; d < LANES * FIRST; d <<= 1) s += __shfl_xor(s, d, 64);
@@ -72,25 +78,20 @@ __device__ __forceinline__ LossPair loss_pair(const float (&t)[C])
 }
 
 // The column of a row's label (outside [0, N): in another piece), -1 of a row without one.
+__device__ __forceinline__ int64_t column_of_label(const LossArgs& o, int64_t y) { return y < 0 ? -1 : y < o.first ? -2 : y - o.first; }
 __device__ __forceinline__ int64_t label_column(const LossArgs& o, int64_t row)
 {
-    const int64_t y = o.labels[row];
-    return y < 0 ? -1 : y < o.first ? -2 : y - o.first;
+    return column_of_label(o, o.labels[row]);
 }
 
 // A row's part in its gradient.
 struct LossRow { float lse2, scale, dloss; int64_t label; };     // lse log2(e); dloss (1 + 2 w lse); as above
 
-__device__ __forceinline__ LossRow loss_row(const LossArgs& o, int64_t row)
+__device__ __forceinline__ LossRow loss_row(const LossArgs& o, float lse, float dloss, int64_t label)
 {
-    LossRow r;
-    const float lse = o.lse[row];
-    r.lse2 = lse * kLog2e;
-    r.dloss = o.dloss[o.dloss_per_row ? row : 0];
-    r.scale = o.z_weight != 0.0f ? r.dloss * __builtin_fmaf(2.0f * o.z_weight, lse, 1.0f) : r.dloss;
-    r.label = label_column(o, row);
-    return r;
+    return {lse * kLog2e, o.z_weight != 0.0f ? dloss * __builtin_fmaf(2.0f * o.z_weight, lse, 1.0f) : dloss, dloss, column_of_label(o, label)};
 }
+__device__ __forceinline__ LossRow loss_row(const LossArgs& o, int64_t row) { return loss_row(o, o.lse[row], o.dloss[o.dloss_per_row ? row : 0], o.labels[row]); }
 
 // x: t - lse2 of G rows of W columns -> the gradient, stored; scale, dloss, label: of the rows (label as above, of any integer type).  Returns the largest magnitude.
 template <int G, int W, class I>

@@ -8,18 +8,58 @@
 namespace fp8mm {
 namespace {
 
+// What the tile's end needs of a lane's four rows, asked for while the last stage is multiplied (registers of the stage before are free then).
+template <int NB, int OP>
+struct LossRows {
+    int64_t label[4];
+    float lse[4], dloss[4];
+    __device__ __forceinline__ void fetch(const LossArgs& o, int M, int m0, int w)
+    {
+        const int l = (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+#pragma unroll
+        for (int mb = 0; mb < 4; ++mb) {
+            const int row = min(m0 + (w >> 1) * 128 + mb * 32 + (l & 31), M - 1);
+            label[mb] = o.labels[row];
+            if (OP == 5) { lse[mb] = o.lse[row]; dloss[mb] = o.dloss[o.dloss_per_row ? row : 0]; }
+        }
+    }
+};
+template <int NB> struct OpTouch<NB, 4> : LossRows<NB, 4> { };
+template <int NB> struct OpTouch<NB, 5> : LossRows<NB, 5> { };
+
+// The sums of the wave's rows 32 mb .. 32 mb + 31.  (The ends below walk the four blocks of rows in a loop: unrolled, a tile's end was four times the code, which
+// every tile fetches anew.)
+template <int NB>
+__device__ __forceinline__ void sums_of(const v16f (&acc)[NB][4], int mb, float (&x)[NB * 16])
+{
+    // (the empty statement, another one at the end of each branch, keeps the branches apart: joined they would read the sums by an index, from memory)
+    auto take = [&](auto tag) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < NB * 16; ++i) x[i] = acc[i >> 4][decltype(tag)::value][i & 15];
+        asm volatile("; rows %1" : "+v"(x[0]) : "n"(32 * decltype(tag)::value));
+    };
+    switch (mb) {
+        case 0: take(std::integral_constant<int, 0>{}); break;
+        case 1: take(std::integral_constant<int, 1>{}); break;
+        case 2: take(std::integral_constant<int, 2>{}); break;
+        default: take(std::integral_constant<int, 3>{}); break;
+    }
+}
+// One of a lane's four values.
+template <class T> __device__ __forceinline__ T row_of(const T (&v)[4], int mb) { return mb == 0 ? v[0] : mb == 1 ? v[1] : mb == 2 ? v[2] : v[3]; }
+// The column of a lane's value i of its row, of lanes h = 0 .. 31 and 32 .. 63.
+__device__ __forceinline__ int loss_column(int i, int h) { return (i >> 4) * 32 + ((i >> 2) & 3) * 8 + 4 * h + (i & 3); }
+
 // The loss: straight from the registers.  A lane holds half of a row's columns in each of its four rows (lane l and l + 32 the two halves), so a
 // row's pair over the wave's columns takes one exchange between lanes, and no logit goes through LDS.
-template <int NB>
-__device__ __forceinline__ void loss_store_pairs(v16f (&acc)[NB][4], uint8_t* smem, const LossArgs& o, int M, int N, int m0, int n0, int w)
+// PLAIN: one positive factor for all, no columns outside.
+template <int NB, bool PLAIN>
+__device__ __forceinline__ void loss_store_pairs(v16f (&acc)[NB][4], uint8_t* smem, const LossArgs& o, const LossRows<NB, 4>& rows, double a_all, double b_all, int M, int N, int wave_m0,
+                                                 int wave_n0, int w, int l)
 {
-    const int l = (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));      // (see store_tile)
-    const int h = l >> 5, wave_m0 = m0 + (w >> 1) * 128, wave_n0 = n0 + (w & 1) * (32 * NB);
-    if (wave_n0 >= N) return;
-    const bool inside = wave_n0 + 32 * NB <= N, uniform = !o.a_per_row && o.b_factors == B_ONE;
-    const double a_all = o.a_per_row ? 1.0 : 1.0 / (double)op_scalar(o.sA_dev), b_all = o.b_factors == B_ONE ? 1.0 / (double)op_scalar(o.sB_dev) : 1.0;
+    const int h = l >> 5;
     double* columns = (double*)(smem + OP_COLUMN_FACTORS) + w * 128;
-    if (o.b_factors != B_ONE) {
+    if (!PLAIN && o.b_factors != B_ONE) {
 #pragma unroll
         for (int i = 0; i < (NB + 1) / 2; ++i)
             if (64 * i + l < 32 * NB) *LDS_PTR(double, columns + 64 * i + l) = 1.0 / (double)o.sB_dev[min(wave_n0 + 64 * i + l, N - 1)];
@@ -29,133 +69,158 @@ __device__ __forceinline__ void loss_store_pairs(v16f (&acc)[NB][4], uint8_t* sm
     LossPair* pairs = (LossPair*)o.partials + block * M;
     float* targets = loss_targets(o, M, N);
     const float f = (float)(a_all * b_all), f2 = (float)(a_all * b_all * (double)kLog2e);
-    auto row_block = [&](auto tag) __attribute__((always_inline)) {
-        constexpr int MB = decltype(tag)::value;
-        const int row = wave_m0 + 32 * MB + (l & 31), at = min(row, M - 1);
-        const int64_t label = label_column(o, at) - wave_n0;
-        const double fa = o.a_per_row ? 1.0 / (double)o.sA_dev[at] : a_all * b_all;
+#pragma unroll 1
+    for (int mb = 0; mb < 4; ++mb) {
+        const int row = wave_m0 + 32 * mb + (l & 31);
+        const int64_t from = column_of_label(o, row_of(rows.label, mb)) - wave_n0;
+        const int label = from >= 0 && from < min(32 * NB, N - wave_n0) ? (int)from : -1;
         float t[NB * 16];
+        sums_of<NB>(acc, mb, t);
+        if (!PLAIN) {
+            const double fa = o.a_per_row ? 1.0 / (double)o.sA_dev[min(row, M - 1)] : a_all;
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) t[nb * 16 + e] = acc[nb][MB][e];
-        if (!uniform) {
-#pragma unroll
-            for (int i = 0; i < NB * 16; ++i) {
-                const int c = (i >> 4) * 32 + ((i >> 2) & 3) * 8 + 4 * h + (i & 3);
-                const double fb = o.b_factors == B_ONE ? (o.a_per_row ? b_all : 1.0) : *LDS_PTR(double, columns + c);
-                t[i] *= (float)((o.a_per_row || o.b_factors == B_ONE ? fa : a_all) * fb);
-            }
+            for (int i = 0; i < NB * 16; ++i) t[i] *= (float)(fa * (o.b_factors == B_ONE ? b_all : *LDS_PTR(double, columns + loss_column(i, h))));
         }
-        // the label's column is in few of the tiles: its logit, from the same factor
-        if (__any(label >= 0 && label < 32 * NB)) {
+        // the label's column is in few of the tiles: its logit, by the same factor
+        if (__any(label >= 0)) {
             float z = 0.0f;
 #pragma unroll
-            for (int i = 0; i < NB * 16; ++i) z = label == (i >> 4) * 32 + ((i >> 2) & 3) * 8 + 4 * h + (i & 3) ? t[i] : z;
-            if (label >= 0 && label < 32 * NB && wave_n0 + label < N && ((label >> 2) & 1) == h && row < M) targets[row] = uniform ? z * f : z;
+            for (int i = 0; i < NB * 16; ++i) z = label == loss_column(i, h) ? t[i] : z;
+            if (label >= 0 && ((label >> 2) & 1) == h && row < M) targets[row] = PLAIN ? z * f : z;
         }
-        const float g = uniform ? f2 : kLog2e;
+        if (!PLAIN) {
 #pragma unroll
-        for (int i = 0; i < NB * 16; ++i) t[i] *= g;
-        if (!inside) {
-#pragma unroll
-            for (int i = 0; i < NB * 16; ++i) t[i] = wave_n0 + (i >> 4) * 32 + ((i >> 2) & 3) * 8 + 4 * h + (i & 3) < N ? t[i] : -__builtin_inff();
+            for (int i = 0; i < NB * 16; ++i) t[i] = wave_n0 + loss_column(i, h) < N ? t[i] : -__builtin_inff();
         }
-        const LossPair p = loss_pair<NB * 16, 2, 32>(t);
+        const LossPair p = loss_pair<NB * 16, 2, 32>(t, PLAIN ? f2 : kLog2e);
         if (l < 32 && row < M) pairs[row] = p;
-    };
-    row_block(std::integral_constant<int, 0>{});
-    row_block(std::integral_constant<int, 1>{});
-    row_block(std::integral_constant<int, 2>{});
-    row_block(std::integral_constant<int, 3>{});
+    }
 }
 
-// The gradient: turned around through LDS as by op_store_rows, behind which a lane has eight columns of a row; the rows' parts (LossRow) lie in LDS.
 template <int NB>
-__device__ __forceinline__ void loss_store_gradient(v16f (&acc)[NB][4], uint8_t* smem, const LossArgs& o, void* D, int M, int N, int m0, int n0, int w)
+__device__ __forceinline__ void loss_store_pairs(v16f (&acc)[NB][4], uint8_t* smem, const LossArgs& o, const LossRows<NB, 4>& rows, int M, int N, int m0, int n0, int w)
 {
-    constexpr int WN = 32 * NB, ROWB = WN * 4 + 16, MBS = NB == 4 ? 1 : 2, LANES = WN / 8, ROWS = 64 / LANES, G = 4;
-    constexpr int STEPS = 32 * MBS / (ROWS * G), TURNS = 4 / MBS;
-    static_assert(4 * 32 * MBS * ROWB <= OP_RING && OP_RING + 4 * 128 * 16 <= OP_ROW_FACTORS, "room for the turned rows and the rows' parts");
     const int l = (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));      // (see store_tile)
-    const int h = l >> 5;
-    const int wave_m0 = m0 + (w >> 1) * 128, wave_n0 = n0 + (w & 1) * WN;
-    const int col = wave_n0 + (l % LANES) * 8, left = N - col;
-    uint8_t* blk = smem + w * (32 * MBS * ROWB);
-    uint8_t* parts = smem + OP_RING + w * (128 * 16);
-    double* row_factors = (double*)(smem + OP_ROW_FACTORS) + w * 128;
-    double* column_factors = (double*)(smem + OP_COLUMN_FACTORS) + w * 128 + (l % LANES) * 8;
+    const int wave_m0 = m0 + (w >> 1) * 128, wave_n0 = n0 + (w & 1) * (32 * NB);
+    if (wave_n0 >= N) return;
+    const double a_all = o.a_per_row ? 1.0 : 1.0 / (double)op_scalar(o.sA_dev), b_all = o.b_factors == B_ONE ? 1.0 / (double)op_scalar(o.sB_dev) : 1.0;
+    // (the largest logit belongs to the largest sum where the factor is positive)
+    if (wave_n0 + 32 * NB <= N && !o.a_per_row && o.b_factors == B_ONE && a_all * b_all > 0.0) loss_store_pairs<NB, true>(acc, smem, o, rows, a_all, b_all, M, N, wave_m0, wave_n0, w, l);
+    else loss_store_pairs<NB, false>(acc, smem, o, rows, a_all, b_all, M, N, wave_m0, wave_n0, w, l);
+}
+
+// The gradient: as the plain epilogue leaves outputs, everything in the registers that hold the sums, where a lane's row is one of four, and converted before the
+// turn through LDS, which then moves 4, 2 or 1 bytes an output.  (Turned around as 32-bit sums, with the rows' parts read from LDS for eight columns at a time, as
+// the feed-forward operators do: 4096 x 50257 x 2048 to E5M2 754 us.)
+// UNIFORM: one factor for all.
+template <int OUT, int NB, bool UNIFORM>
+__device__ __forceinline__ void loss_store_gradient(v16f (&acc)[NB][4], uint8_t* smem, const LossArgs& o, const LossRows<NB, 5>& rows, void* D, int M, int N, int m0, int n0, int w)
+{
+    constexpr bool FP8OUT = OUT == OUT_E4M3 || OUT == OUT_E5M2;
+    constexpr int FMT = OUT == OUT_E5M2 ? FP8_E5M2 : FP8_E4M3, ESZ = OUT == OUT_F32 ? 4 : OUT == OUT_BF16 ? 2 : 1;
+    constexpr int WN = 32 * NB, ROWB = WN * ESZ + 16, LANES = WN * ESZ / 16, ROWS = 64 / LANES;      // of the turned block: bytes of a row, its lanes, rows a store
+    static_assert(4 * 32 * ROWB <= OP_COLUMN_FACTORS && 64 % LANES == 0 && 32 % ROWS == 0, "room for the turned rows; whole rows");
+    const int l = (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));      // (see store_tile)
+    const int h = l >> 5, wave_m0 = m0 + (w >> 1) * 128, wave_n0 = n0 + (w & 1) * WN;
+    const bool n_edge = wave_n0 + WN > N;
+    const double a_all = o.a_per_row ? 1.0 : 1.0 / (double)op_scalar(o.sA_dev), b_all = o.b_factors == B_ONE ? 1.0 / (double)op_scalar(o.sB_dev) : 1.0;
+    const float f2 = (float)(a_all * b_all * (double)kLog2e);
+    double* columns = (double*)(smem + OP_COLUMN_FACTORS) + w * 128;
+    if (!UNIFORM && o.b_factors != B_ONE) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const LossRow r = loss_row(o, min(wave_m0 + 64 * i + l, M - 1));
-        const int label = r.label >= 0 && r.label < N ? (int)r.label : r.label == -1 ? -1 : -2;
-        *LDS_PTR(v4f, parts + (64 * i + l) * 16) = (v4f){-r.lse2, r.scale, r.dloss, as_f32((unsigned)label)};
-        if (o.a_per_row) *LDS_PTR(double, row_factors + 64 * i + l) = 1.0 / (double)o.sA_dev[min(wave_m0 + 64 * i + l, M - 1)];
+        for (int i = 0; i < (NB + 1) / 2; ++i)
+            if (64 * i + l < WN) *LDS_PTR(double, columns + 64 * i + l) = 1.0 / (double)o.sB_dev[min(wave_n0 + 64 * i + l, N - 1)];
     }
-    float f[8];
-    {
-        const double a_all = o.a_per_row ? 1.0 : 1.0 / (double)op_scalar(o.sA_dev);
-        const bool one = o.b_factors == B_ONE;
-        const double b_all = one ? 1.0 / (double)op_scalar(o.sB_dev) : 0.0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const double y = (one ? b_all : op_column_factor(o, N, min(col + i, N - 1), false)) * (double)kLog2e;
-            f[i] = (float)(a_all * y);
-            if (o.a_per_row) *LDS_PTR(double, column_factors + i) = y;
-        }
-    }
-    const float sD = o.out_kind >= OUT_E4M3 && o.sD_dev ? op_scalar(o.sD_dev) : 1.0f;
-    const bool inside = wave_m0 + 128 <= M && wave_n0 + WN <= N;
+    const float sD = FP8OUT && o.sD_dev ? op_scalar(o.sD_dev) : 1.0f;
+    uint8_t* blk = smem + w * (32 * ROWB);
+    uint8_t* d_wave = (uint8_t*)D + ((size_t)wave_m0 * N + wave_n0) * ESZ;
+    const int st_row = l / LANES, st_col = (l % LANES) * 16, left = N - (wave_n0 + st_col / ESZ);
     unsigned top = 0;
-#pragma unroll 1
-    for (int turn = 0; turn < TURNS; ++turn) {
-        auto turn_rows = [&](auto turn_tag) __attribute__((always_inline)) {
-            constexpr int T = decltype(turn_tag)::value;
-            if constexpr (T < TURNS) {
 #pragma unroll
-                for (int mb = 0; mb < MBS; ++mb)
+    for (int mb = 0; mb < 4; ++mb) {
+        const LossRow part = loss_row(o, row_of(rows.lse, mb), row_of(rows.dloss, mb), row_of(rows.label, mb));
+        const int row = wave_m0 + mb * 32 + (l & 31);
+        const bool none = part.label == -1;
+        // (of a row without a label 2^-infinity times 0; what is infinite or NaN itself is taken out below)
+        const float nlse2 = none ? -__builtin_inff() : -part.lse2, scale = none ? 0.0f : part.scale;
+        const int64_t from = part.label - wave_n0;
+        const int label = from >= 0 && from < WN ? (int)from : -1;
+        float x[NB * 16];
 #pragma unroll
-                    for (int nb = 0; nb < NB; ++nb)
+        for (int i = 0; i < NB * 16; ++i) x[i] = acc[i >> 4][mb][i & 15];
+        if (!UNIFORM) {
+            const double fa = o.a_per_row ? 1.0 / (double)o.sA_dev[min(row, M - 1)] : a_all;
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            const v16f& a = acc[nb][T * MBS + mb];
-                            *LDS_PTR(v4f, blk + (mb * 32 + (l & 31)) * ROWB + (nb * 32 + 8 * q + 4 * h) * 4) = (v4f){a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3]};
-                        }
-            }
-        };
-        switch (turn) {
-            case 0: turn_rows(std::integral_constant<int, 0>{}); break;
-            case 1: turn_rows(std::integral_constant<int, 1>{}); break;
-            case 2: turn_rows(std::integral_constant<int, 2>{}); break;
-            default: turn_rows(std::integral_constant<int, 3>{}); break;
+            for (int i = 0; i < NB * 16; ++i) x[i] *= (float)(fa * (o.b_factors == B_ONE ? b_all : *LDS_PTR(double, columns + loss_column(i, h))));
         }
-#pragma unroll 1
-        for (int in_turn = 0; in_turn < STEPS; ++in_turn) {
-            const int i = turn * STEPS + in_turn;
-            float x[G * 8], scale[G], dloss[G];
-            int label[G];
-            OutRows<G> t;
-            t.col = col; t.left = left; t.rows = 0; t.whole = inside;
+        unsigned row_top = 0;
 #pragma unroll
-            for (int g = 0; g < G; ++g) {
-                const int in_wave = (i * G + g) * ROWS + l / LANES, row = wave_m0 + in_wave;
-                const uint8_t* src = blk + ((in_turn * G + g) * ROWS + l / LANES) * ROWB + (l % LANES) * 32;
-                const v4f part = *LDS_PTR(v4f, parts + in_wave * 16);
-                scale[g] = part[1]; dloss[g] = part[2]; label[g] = (int)as_u32(part[3]);
-                const double fa = o.a_per_row ? *LDS_PTR(double, row_factors + in_wave) : 1.0;
+        for (int nb = 0; nb < NB; ++nb) {
+            float y[16];
 #pragma unroll
-                for (int p = 0; p < 2; ++p) {
-                    const v4f s = *LDS_PTR(v4f, src + 16 * p);
+            for (int i = 0; i < 16; ++i) y[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[nb * 16 + i], UNIFORM ? f2 : kLog2e, nlse2)) * scale;
+            if (__any(label >> 5 == nb)) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float factor = o.a_per_row ? (float)(fa * *LDS_PTR(double, column_factors + 4 * p + e)) : f[4 * p + e];
-                        x[8 * g + 4 * p + e] = __builtin_fmaf(s[e], factor, part[0]);
+                for (int i = 0; i < 16; ++i) y[i] = label == loss_column(nb * 16 + i, h) ? y[i] - part.dloss : y[i];
+            }
+            unsigned most = max_bits_of<16>(y);
+            if (__any(none && most != 0)) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) y[i] = none ? 0.0f : y[i];
+                most = none ? 0u : most;
+            }
+            if (n_edge && o.amax_out) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) row_top = max(row_top, wave_n0 + loss_column(nb * 16 + i, h) < N ? as_u32(y[i]) & 0x7fffffffu : 0u);
+            } else {
+                row_top = max(row_top, most);
+            }
+            uint8_t* dst = blk + (l & 31) * ROWB + (nb * 32 + 4 * h) * ESZ;
+            if (OUT == OUT_F32) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) *LDS_PTR(v4f, dst + 8 * q * ESZ) = (v4f){y[4 * q], y[4 * q + 1], y[4 * q + 2], y[4 * q + 3]};
+            } else if (OUT == OUT_BF16) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    v2i p;
+                    p.x = (int)__builtin_bit_cast(unsigned, __builtin_convertvector((v2f){y[4 * q], y[4 * q + 1]}, v2bf));
+                    p.y = (int)__builtin_bit_cast(unsigned, __builtin_convertvector((v2f){y[4 * q + 2], y[4 * q + 3]}, v2bf));
+                    *LDS_PTR(v2i, dst + 8 * q * ESZ) = p;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) y[i] *= sD;
+                // (as in the plain epilogue: the largest product tells whether anything has to be clamped or looked at)
+                u32x4 p;
+                if (__all(__builtin_fabsf(as_f32(most) * sD) <= (FMT == FP8_E4M3 ? 448.0f : 57344.0f))) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) p[q] = encode4_inside<FMT>(y[4 * q], y[4 * q + 1], y[4 * q + 2], y[4 * q + 3]);
+                } else {
+                    p = encode16<FMT, kCastCvt>(y);
+                }
+#pragma unroll
+                for (int q = 0; q < 4; ++q) *LDS_PTR(unsigned, dst + 8 * q) = p[q];
+            }
+        }
+        if (row < M) top = max(top, row_top);
+#pragma unroll
+        for (int i = 0; i < 32 / ROWS; ++i) {
+            const int r = i * ROWS + st_row;
+            if (wave_m0 + mb * 32 + r >= M || left <= 0) continue;                         // beyond the edges of D
+            uint8_t* out = d_wave + (size_t)(mb * 32 + r) * N * ESZ + st_col;
+            const u32x4 p = *LDS_PTR(u32x4, blk + r * ROWB + st_col);
+            if (left >= 16 / ESZ) {
+                __builtin_nontemporal_store(p, (u32x4_any*)out);
+            } else {                                        // the end of a row inside the lane's 16 bytes
+#pragma unroll
+                for (int e = 0; e < 16 / ESZ - 1; ++e) {
+                    if (e < left) {
+                        if (ESZ == 4) ((unsigned*)out)[e] = p[e & 3];
+                        else if (ESZ == 2) ((unsigned short*)out)[e] = (unsigned short)(p[(e >> 1) & 3] >> (16 * (e & 1)));
+                        else out[e] = (uint8_t)(p[e >> 2] >> (8 * (e & 3)));
                     }
                 }
-                t.row[g] = row;
-                if (row < M && left > 0) t.rows |= 1u << g;
             }
-            top = max(top, loss_grad_finish<G, 8>(o, D, N, t, x, scale, dloss, label, sD));
         }
     }
     if (o.amax_out) {
@@ -164,16 +229,32 @@ __device__ __forceinline__ void loss_store_gradient(v16f (&acc)[NB][4], uint8_t*
         unsigned* cells = (unsigned*)(smem + OP_AMAX);
         if (l == 0) *LDS_PTR(unsigned, cells + w) = top;
         __syncthreads();
-        if (w == 0) op_commit_top(o, l < 4 ? *LDS_PTR(unsigned, cells + l) : 0u);
+        // (unasked: 256 workgroups that end together queue up for a look at the cell longer than for the atomic itself, whose end nobody waits for)
+        if (w == 0 && l == 0) {
+            const u32x4 all = *LDS_PTR(u32x4, cells);
+            atomicMax((unsigned*)o.amax_out, max(max(all[0], all[1]), max(all[2], all[3])));
+        }
     }
+}
+
+template <int OUT, int NB>
+__device__ __forceinline__ void loss_store_gradient(v16f (&acc)[NB][4], uint8_t* smem, const LossArgs& o, const LossRows<NB, 5>& rows, void* D, int M, int N, int m0, int n0, int w)
+{
+    if (!o.a_per_row && o.b_factors == B_ONE) loss_store_gradient<OUT, NB, true>(acc, smem, o, rows, D, M, N, m0, n0, w);
+    else loss_store_gradient<OUT, NB, false>(acc, smem, o, rows, D, M, N, m0, n0, w);
 }
 
 // OP of the tile: 4 the loss, 5 its gradient.
 template <int NB, int OP>
-__device__ __forceinline__ void loss_store_tile(v16f (&acc)[NB][4], uint8_t* smem, const LossArgs& o, void* D, int M, int N, int m0, int n0, int w)
+__device__ __forceinline__ void loss_store_tile(v16f (&acc)[NB][4], uint8_t* smem, const LossArgs& o, const LossRows<NB, OP>& rows, void* D, int M, int N, int m0, int n0, int w)
 {
-    if constexpr (OP == 4) loss_store_pairs<NB>(acc, smem, o, M, N, m0, n0, w);
-    else loss_store_gradient<NB>(acc, smem, o, D, M, N, m0, n0, w);
+    if constexpr (OP == 4) loss_store_pairs<NB>(acc, smem, o, rows, M, N, m0, n0, w);
+    else switch (o.out_kind) {
+        case OUT_F32: loss_store_gradient<OUT_F32, NB>(acc, smem, o, rows, D, M, N, m0, n0, w); break;
+        case OUT_BF16: loss_store_gradient<OUT_BF16, NB>(acc, smem, o, rows, D, M, N, m0, n0, w); break;
+        case OUT_E4M3: loss_store_gradient<OUT_E4M3, NB>(acc, smem, o, rows, D, M, N, m0, n0, w); break;
+        default: loss_store_gradient<OUT_E5M2, NB>(acc, smem, o, rows, D, M, N, m0, n0, w); break;
+    }
 }
 
 }  // namespace

@@ -27,8 +27,10 @@
 // 8192 x 12288 x 4095 (both contiguous along K) 884 -> 694, 5000 x 5001 x 5001 with A stored K x M 624 -> 274;
 // 256 x 128: 4673 x 4573 x 1057 147 -> 72, 1307 x 12288 x 4405 to E4M3 256 -> 223.
 //
-// This file is compiled once per pair of storage orders: -DFP8MM_LAYOUT.
+// This file is compiled once per pair of storage orders, -DFP8MM_LAYOUT, and again with -DFP8MM_LOSS for the loss over a vocabulary and its gradient
+// (gemm_loss_epilogue.hpp; operands in E4M3).
 #include "gemm_epilogue.hpp"
+#include "gemm_loss_epilogue.hpp"
 #include "gemm_slabs.hpp"
 
 #include <atomic>
@@ -139,10 +141,11 @@ constexpr int any_lds()
     return slabs > EP_AMAX + 1024 ? slabs : EP_AMAX + 1024;
 }
 
-template <int FMT_A, int FMT_B, bool A_KC, bool B_KC, int NB>
+// OP: 0 the plain product, 4 the loss, 5 its gradient (ep: a LossArgs).
+template <int FMT_A, int FMT_B, bool A_KC, bool B_KC, int NB, int OP>
 __global__ __launch_bounds__(256, 1) void gemm_mfma_any_kernel(
     const uint8_t* __restrict__ A, const uint8_t* __restrict__ B, void* __restrict__ C,
-    int64_t M, int64_t N, int64_t K, EpilogueArgs ep)
+    int64_t M, int64_t N, int64_t K, typename std::conditional<OP == 0, EpilogueArgs, LossArgs>::type ep)
 {
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
     typedef Staged<A_KC, 256> StagedA;
@@ -296,22 +299,25 @@ __global__ __launch_bounds__(256, 1) void gemm_mfma_any_kernel(
         step(yes, yes, s + 1, 1, af1, bf1, af0, bf0);
     }
     step(no, no, s, 0, af0, bf0, af1, bf1);
+    [[maybe_unused]] OpTouch<NB, OP> rows = {};
+    if constexpr (OP >= 4) rows.fetch(ep, (int)M, (int)m0, w);
 #pragma unroll
     for (int j = 0; j < P; ++j) {
         compute(j);
         if (j + 1 < P) convert(j + 1, af1, bf1);
     }
     __syncthreads();                                  // every wave is done with the slabs
-    store_tile<NB, true>(acc, smem, ep, C, (int)M, (int)N, (int)m0, (int)n0, w);
+    if constexpr (OP >= 4) loss_store_tile<NB, OP>(acc, smem, ep, rows, C, (int)M, (int)N, (int)m0, (int)n0, w);
+    else store_tile<NB, true>(acc, smem, ep, C, (int)M, (int)N, (int)m0, (int)n0, w);
 }
 
-template <int FA, int FB, bool A_KC, bool B_KC, int NB>
-int launch_tile(const GemmArgs& g)
+template <int FA, int FB, bool A_KC, bool B_KC, int NB, int OP, class ARGS>
+int launch_tile(const GemmArgs& g, const ARGS& ep)
 {
-    // more dynamic LDS than the default limit: raised once per device
-    constexpr int LDS = any_lds<A_KC, B_KC, NB>();
+    // more dynamic LDS than the default limit: raised once per device (the ends of the loss use all of it)
+    constexpr int LDS = OP == 0 ? any_lds<A_KC, B_KC, NB>() : 160 * 1024;
     static std::atomic<unsigned long long> attr_set{0ull};
-    auto kern = gemm_mfma_any_kernel<FA, FB, A_KC, B_KC, NB>;
+    auto kern = gemm_mfma_any_kernel<FA, FB, A_KC, B_KC, NB, OP>;
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess) return fail(FP8_ERR_DEVICE, "hipGetDevice failed");
     const unsigned long long bit = 1ull << (dev & 63);
@@ -322,14 +328,14 @@ int launch_tile(const GemmArgs& g)
         if (dev < 64) attr_set.fetch_or(bit, std::memory_order_relaxed);
     }
     const int64_t tiles = ((g.M + 255) / 256) * ((g.N + 64 * NB - 1) / (64 * NB));
-    enqueue(kern, dim3((unsigned)tiles), dim3(256), LDS, g.stream, g.A, g.B, g.C, g.M, g.N, g.K, g.ep);
+    enqueue(kern, dim3((unsigned)tiles), dim3(256), LDS, g.stream, g.A, g.B, g.C, g.M, g.N, g.K, ep);
     return check_launch("gemm (matrix-core kernel for any shape)");
 }
 
 template <int FA, int FB, bool A_KC, bool B_KC>
 int launch_one(const GemmArgs& g, int width)
 {
-    return width == 256 ? launch_tile<FA, FB, A_KC, B_KC, 4>(g) : launch_tile<FA, FB, A_KC, B_KC, 2>(g);
+    return width == 256 ? launch_tile<FA, FB, A_KC, B_KC, 4, 0>(g, g.ep) : launch_tile<FA, FB, A_KC, B_KC, 2, 0>(g, g.ep);
 }
 
 }  // namespace
@@ -338,6 +344,16 @@ int launch_one(const GemmArgs& g, int width)
 #error "compile with -DFP8MM_LAYOUT=0..3 (2 * transA + transB)"
 #endif
 
+#if defined(FP8MM_LOSS)
+#define FP8MM_LOSS_ANY_NAME_(l) launch_loss_any_l##l
+#define FP8MM_LOSS_ANY_NAME(l) FP8MM_LOSS_ANY_NAME_(l)
+int FP8MM_LOSS_ANY_NAME(FP8MM_LAYOUT)(const GemmArgs& g, const LossArgs& o, int width)
+{
+    constexpr bool A_KC = (FP8MM_LAYOUT & 2) == 0, B_KC = (FP8MM_LAYOUT & 1) != 0;
+    if (o.op == OP_LOSS) return width == 256 ? launch_tile<FP8_E4M3, FP8_E4M3, A_KC, B_KC, 4, 4>(g, o) : launch_tile<FP8_E4M3, FP8_E4M3, A_KC, B_KC, 2, 4>(g, o);
+    return width == 256 ? launch_tile<FP8_E4M3, FP8_E4M3, A_KC, B_KC, 4, 5>(g, o) : launch_tile<FP8_E4M3, FP8_E4M3, A_KC, B_KC, 2, 5>(g, o);
+}
+#else
 // This file is compiled once per pair of storage orders (-DFP8MM_LAYOUT): A stored M x K is
 // K-contiguous, B stored N x K (transB) is K-contiguous.
 int FP8MM_ANY_NAME(FP8MM_LAYOUT)(const GemmArgs& g, int width)
@@ -347,5 +363,6 @@ int FP8MM_ANY_NAME(FP8MM_LAYOUT)(const GemmArgs& g, int width)
         return g.fmtB == FP8_E4M3 ? launch_one<FP8_E4M3, FP8_E4M3, A_KC, B_KC>(g, width) : launch_one<FP8_E4M3, FP8_E5M2, A_KC, B_KC>(g, width);
     return g.fmtB == FP8_E4M3 ? launch_one<FP8_E5M2, FP8_E4M3, A_KC, B_KC>(g, width) : launch_one<FP8_E5M2, FP8_E5M2, A_KC, B_KC>(g, width);
 }
+#endif
 
 }  // namespace fp8mm

@@ -176,8 +176,9 @@ __global__ __launch_bounds__(256) void column_sum_kernel(const float* __restrict
 }
 
 // Which kernel takes the call: the one of few rows where it pays, else what the plain product of the same operands takes, as far as it exists with these ends
-// (not the any-shape kernel, tiles of 192 columns or the persistent form).
-struct OpPlan { bool generic, tiled; int small, acc, tile_n, wide_cols; bool skinny; };
+// (not tiles of 192 columns or the persistent form, the any-shape kernel for the loss only).
+// any: the any-shape kernel, which exists for the loss; its tiles are tile_n wide.
+struct OpPlan { bool generic, tiled; int small, acc, tile_n, wide_cols; bool skinny; bool any = false; };
 OpPlan plan_op(const GemmArgs& g, const OpArgs& o)
 {
     const bool pair = op_pair_in(o.op);
@@ -202,11 +203,14 @@ OpPlan plan_op(const GemmArgs& g, const OpArgs& o)
     // The tiled kernel exists for a weight in E4M3 (the format of weights); E5M2, and shapes and alignments that it does not take, go to tiles of 64 x 64 (4096 x 6144 x
     // 2048 with GELU 108 us, in E5M2 171; with K = 2047 226; up to some hundreds of tiles as fast as the plain product).
     const bool tiled = plan.kernel != GEMM_MFMA_ANY && g.fmtB == FP8_E4M3 && halves && !(loss && (g.transA || wide_formats)) && (!pair || !g.transB || (uint64_t)(g.N + TILE_M) * (uint64_t)g.K < (1ull << 32));
+    if (loss && !tiled && !wide_formats) {
+        if (const int width = mfma_any_width(p)) return {false, false, SMALL_NONE, (int)ACC_F16, width, 0, false, true};
+    }
     if (!tiled) return ((g.M + 63) / 64) * ((p.N + 63) / 64) > 0x7fffffffll ? plain_fmas : OpPlan{false, false, SMALL_64x64, acc, 0, 0, false};
     // The width whose rounds of 256 workgroups take less time, or both widths in one launch, by the plain product's model of run times with the
     // operator's own time on top (us of a 256-wide tile: fitted to 8192 x 8192 outputs over K = 256; it is the same per output in both widths).
     const TileTimes t = tile_times(acc, 2.0 * (double)((g.K + 2 * TILE_K - 1) / (2 * TILE_K)));
-    const double own = loss ? 7.0 : o.op == OP_GATED_GRAD ? 25.0 : o.op == OP_GATED ? 3.0 : o.op == OP_ACT_GRAD || o.side ? 12.0 : 7.0;
+    const double own = o.op == OP_LOSS ? 1.0 : loss ? 10.0 : o.op == OP_GATED_GRAD ? 25.0 : o.op == OP_GATED ? 3.0 : o.op == OP_ACT_GRAD || o.side ? 12.0 : 7.0;
     const double wide = t.wide + own, narrow = t.narrow + 0.5 * own;
     const int64_t tiles_m = (g.M + TILE_M - 1) / TILE_M, wide_all = (p.N + 255) / 256, narrow_all = (p.N + 127) / 128;
     const double us_wide = tiles_makespan(tiles_m * wide_all, 0, wide, narrow), us_narrow = tiles_makespan(0, tiles_m * narrow_all, wide, narrow);
@@ -219,7 +223,8 @@ OpPlan plan_op(const GemmArgs& g, const OpArgs& o)
         return r;
     }
     // (as many wide columns as whole rounds hold: fewer or more leave units idle between the widths; beyond 16 rounds the last one matters little)
-    double best = 0.97 * std::min(us_wide, us_narrow);
+    // (the loss by 1.5 % of the model's time: 4096 x 50257 x 2048 639 -> 625 us, its gradient 767 -> 749)
+    double best = (loss ? 0.985 : 0.97) * std::min(us_wide, us_narrow);
     for (int64_t units = 256; units / tiles_m < wide_all && tiles_m * wide_all <= 16 * 256; units += 256) {
         const int64_t c = std::max<int64_t>(units / tiles_m, 1);
         const double us = tiles_makespan(tiles_m * c, tiles_m * ((p.N - c * 256 + 127) / 128), wide, narrow) + 3.0;
@@ -296,6 +301,8 @@ int launch_gemm_loss(const GemmArgs& g, const LossArgs& args, float* loss, float
     typedef int (*small_fn)(const GemmArgs&, const LossArgs&, int);
     static const small_fn small[4] = {launch_loss_small_l0, launch_loss_small_l1, launch_loss_small_l2, launch_loss_small_l3};
     typedef int (*tiled_fn)(const GemmArgs&, const LossArgs&);
+    typedef int (*any_fn)(const GemmArgs&, const LossArgs&, int);
+    static const any_fn any[4] = {launch_loss_any_l0, launch_loss_any_l1, launch_loss_any_l2, launch_loss_any_l3};
     static const tiled_fn tiled[2][2] = {{launch_loss_tiled_l0_a0, launch_loss_tiled_l0_a1}, {launch_loss_tiled_l1_a0, launch_loss_tiled_l1_a1}};
     LossArgs o = args;
     int64_t blocks = 0;                                      // of columns, with a pair each for every row
@@ -308,10 +315,11 @@ int launch_gemm_loss(const GemmArgs& g, const LossArgs& args, float* loss, float
         GemmArgs p = g;
         p.acc = plan.acc; p.tile_n = plan.tile_n; p.wide_cols = o.wide_cols = plan.wide_cols;
         // (a wave of the tiled kernel has half a tile's columns)
-        const int64_t width = plan.tiled ? plan.tile_n / 2 : plan.small == SMALL_32x32 ? 32 : 64;
+        const int order = (g.transA ? 2 : 0) + (g.transB ? 1 : 0);
+        const int64_t width = plan.tiled || plan.any ? plan.tile_n / 2 : plan.small == SMALL_32x32 ? 32 : 64;
         blocks = plan.wide_cols ? 2 * (int64_t)plan.wide_cols + (g.N - 256 * (int64_t)plan.wide_cols + 63) / 64 : (g.N + width - 1) / width;
         if (int e = plan.generic ? launch_generic(g, o) : plan.tiled ? tiled[g.transB][plan.acc == ACC_FP8 ? 1 : 0](p, o)
-                                                                     : small[(g.transA ? 2 : 0) + (g.transB ? 1 : 0)](p, o, plan.small)) return e;
+                           : plan.any ? any[order](p, o, plan.tile_n) : small[order](p, o, plan.small)) return e;
     }
     return o.op == OP_LOSS && g.M > 0 ? launch_loss_join(o, blocks, g.M, g.N, loss, lse, g.stream) : (int)FP8_OK;
 }

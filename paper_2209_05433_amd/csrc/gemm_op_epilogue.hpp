@@ -299,8 +299,6 @@ struct OpTouch {
 };
 template <int NB> struct OpTouch<NB, 0> { };
 template <int NB> struct OpTouch<NB, 2> { };
-template <int NB> struct OpTouch<NB, 4> { };
-template <int NB> struct OpTouch<NB, 5> { };
 
 // OP of the tile: 1 the product alone, 2 the gated block, 3 the gradients.
 template <int NB, int OP>

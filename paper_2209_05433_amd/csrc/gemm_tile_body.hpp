@@ -687,6 +687,7 @@ __device__ __forceinline__ void gemm_tile_body(
         }
     }
     k_step(checked, KT - 2, false, sa, sb, sa, sb, af0, bf0, af1, bf1, no);
+    if constexpr (OP >= 4) beside.fetch(static_cast<const LossArgs&>(ep), M, m0, w);
 #pragma unroll
     for (int j = 0; j < P; ++j) {
         if (ACC == ACC_FP8) {
@@ -704,7 +705,7 @@ __device__ __forceinline__ void gemm_tile_body(
     __builtin_amdgcn_s_waitcnt(0xC07F);
     __builtin_amdgcn_s_barrier();                           // every wave is done with the operand slabs
     if constexpr (OP == 1 || OP == 3) beside.touched();
-    if constexpr (OP >= 4) loss_store_tile<NB, OP>(acc, smem, static_cast<const LossArgs&>(ep), C, M, N, m0, n0, w);
+    if constexpr (OP >= 4) loss_store_tile<NB, OP>(acc, smem, static_cast<const LossArgs&>(ep), beside, C, M, N, m0, n0, w);
     else if constexpr (OP != 0) op_store_tile<NB, OP>(acc, smem, static_cast<const OpArgs&>(ep), C, M, N, m0, n0, w);
     else store_tile<NB, false>(acc, smem, ep, C, M, N, m0, n0, w);
 }

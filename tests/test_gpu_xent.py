@@ -21,7 +21,8 @@ E4M3, E5M2 = fp8.FP8_E4M3, fp8.FP8_E5M2
 TORCH8 = {E4M3: torch.float8_e4m3fn, E5M2: torch.float8_e5m2}
 F32, BF16, O43, O52 = fp8.FP8_OUT_F32, fp8.FP8_OUT_BF16, fp8.FP8_OUT_E4M3, fp8.FP8_OUT_E5M2
 DTYPE = {F32: torch.float32, BF16: torch.bfloat16, O43: torch.uint8, O52: torch.uint8}
-FORMS = {"chosen": {}, "fma": {fp8.FP8_KNOB_GEMM_KERNEL: 1}, "small_32x32": {fp8.FP8_KNOB_SMALL: 2}, "small_32x64": {fp8.FP8_KNOB_SMALL: 3},
+FORMS = {"chosen": {}, "any_256": {fp8.FP8_KNOB_GEMM_KERNEL: 2, fp8.FP8_KNOB_TILE_N: 256},
+         "any_128": {fp8.FP8_KNOB_GEMM_KERNEL: 2, fp8.FP8_KNOB_TILE_N: 128}, "fma": {fp8.FP8_KNOB_GEMM_KERNEL: 1}, "small_32x32": {fp8.FP8_KNOB_SMALL: 2}, "small_32x64": {fp8.FP8_KNOB_SMALL: 3},
          "small_64x64": {fp8.FP8_KNOB_SMALL: 4}, "tiled_256": {fp8.FP8_KNOB_SMALL: 1, fp8.FP8_KNOB_TILE_N: 256},
          "tiled_128": {fp8.FP8_KNOB_SMALL: 1, fp8.FP8_KNOB_TILE_N: 128}, "tiled_both": {fp8.FP8_KNOB_SMALL: 1, fp8.FP8_KNOB_MIXED: 2}}
 
