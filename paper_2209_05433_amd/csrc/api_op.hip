@@ -273,6 +273,7 @@ int fp8_adamw(int count, void* const* p, const int* p_dtype, const void* const* 
     for (int i = 0; i < count; ++i) {
         if (weight_decay && !(weight_decay[i] >= 0.0f && weight_decay[i] < __builtin_inff()))
             return fail(FP8_ERR_INVALID_ARG, "%s: weight_decay[%d] is negative or not finite", who, i);
+        if (n[i] > (size_t)1 << 43) return fail(FP8_ERR_UNSUPPORTED, "%s: tensor %d has more than 2^43 elements", who, i);
         if (n[i] == 0) continue;
         const int state = states8 ? 1 : 4;
         if (!m[i] || !v[i] || (uintptr_t)m[i] % state || (uintptr_t)v[i] % state) return fail(FP8_ERR_INVALID_ARG, "%s: m[%d] or v[%d] is NULL or misaligned", who, i, i);

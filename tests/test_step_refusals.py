@@ -99,7 +99,7 @@ def test_what_adamw_refuses(wrong, word):
 
 
 def test_adamw_sizes():
-    assert adamw(n=(200, (1 << 45) + 1)) == UNSUPPORTED
+    assert adamw(n=(200, (1 << 45) + 1)) == UNSUPPORTED and adamw(n=(200, (1 << 43) + 1)) == UNSUPPORTED
     # nothing to do: no pointer is looked at
     assert adamw(count=0, p=None, g=None, n=None, m=None, v=None, p_dtype=None, g_dtype=None) == fp8.FP8_OK
     assert adamw(n=(0, 0), p=(None, None), g=(None, None), m=(None, None), v=(None, None)) == fp8.FP8_OK
