@@ -227,6 +227,10 @@ int fp8_gemm_xent(const uint8_t* A, int fmtA, int transA, const uint8_t* B, int 
     if (overlap(loss, cells, lse, cells) || overlap(loss, cells, workspace, (int64_t)need) || overlap(lse, cells, workspace, (int64_t)need) ||
         overlap(labels, 8 * M, loss, cells) || overlap(labels, 8 * M, lse, cells) || overlap(labels, 8 * M, workspace, (int64_t)need))
         return fail(FP8_ERR_INVALID_ARG, "%s: loss, lse, the workspace and labels overlap", who);
+    const struct { const void* p; int64_t bytes; } in[] = {{A, bytes_of(M, K, 1)}, {B, bytes_of(K, N, 1)}, {sA_dev, 4 * nsA}, {sB_dev, 4 * nsB}};
+    for (const auto& x : in)
+        if (overlap(loss, cells, x.p, x.bytes) || overlap(lse, cells, x.p, x.bytes) || overlap(workspace, (int64_t)need, x.p, x.bytes))
+            return fail(FP8_ERR_INVALID_ARG, "%s: loss, lse or the workspace overlaps an operand or its factors", who);
     o.partials = workspace;
     return launch_gemm_loss(g, o, loss, lse);
 }

@@ -233,6 +233,18 @@ OpPlan plan_op(const GemmArgs& g, const OpArgs& o)
     return r;
 }
 
+// Whether the plan's workgroups fit a launch, of fewer than 2^32 threads; asked before the first launch of a call.
+int check_grid(const OpPlan& plan, int64_t M, int64_t columns)
+{
+    auto count = [](int64_t n, int64_t per) { return (n + per - 1) / per; };
+    const bool few = plan.small == SMALL_32x32 || plan.small == SMALL_32x64;
+    const int64_t tiles = plan.skinny ? count(columns, 16) : plan.tiled || plan.any ? count(M, TILE_M) * count(columns, 128)
+                                                           : count(M, few ? 32 : 64) * count(columns, plan.small == SMALL_32x32 ? 32 : 64);
+    const int threads = plan.skinny || plan.small == SMALL_32x32 || plan.small == SMALL_64x64_LINES8 ? 512 : 256;
+    if (tiles > (int64_t)UINT32_MAX / threads) return fail(FP8_ERR_UNSUPPORTED, "gemm with an operator: %lld tiles of %d threads exceed the grid limit", (long long)tiles, threads);
+    return FP8_OK;
+}
+
 }  // namespace
 
 int raise_lds_limit(const void* kernel, int bytes, std::atomic<unsigned long long>& done)
@@ -261,6 +273,7 @@ int launch_gemm_op(const GemmArgs& g, const OpArgs& args, float* dbias)
     int64_t parts = 0, tops = 0;                             // rows of partial sums; workgroups that leave their maxima in memory
     if (work) {
         plan = plan_op(g, o);
+        if (int e = check_grid(plan, g.M, op_pair_in(o.op) && !plan.generic ? 2 * g.N : g.N)) return e;
         int64_t rows = 64, width = 64;                       // of a workgroup's outputs
         if (plan.skinny) { rows = 16; width = 16; }
         else if (plan.tiled) { rows = TILE_M; width = plan.tile_n; }
@@ -306,12 +319,16 @@ int launch_gemm_loss(const GemmArgs& g, const LossArgs& args, float* loss, float
     static const tiled_fn tiled[2][2] = {{launch_loss_tiled_l0_a0, launch_loss_tiled_l0_a1}, {launch_loss_tiled_l1_a0, launch_loss_tiled_l1_a1}};
     LossArgs o = args;
     int64_t blocks = 0;                                      // of columns, with a pair each for every row
+    OpPlan plan{};
+    if (g.M > 0 && g.N > 0) {
+        plan = plan_op(g, o);
+        if (int e = check_grid(plan, g.M, g.N)) return e;
+    }
     if (o.amax_out) {                                        // written, not accumulated
         enqueue(op_zero_cell_kernel, dim3(1), dim3(1), 0, g.stream, (unsigned*)o.amax_out);
         if (int e = check_launch("gradient of the loss (amax init)")) return e;
     }
     if (g.M > 0 && g.N > 0) {
-        const OpPlan plan = plan_op(g, o);
         GemmArgs p = g;
         p.acc = plan.acc; p.tile_n = plan.tile_n; p.wide_cols = o.wide_cols = plan.wide_cols;
         // (a wave of the tiled kernel has half a tile's columns)

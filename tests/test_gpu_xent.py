@@ -299,6 +299,43 @@ def test_infinities_and_nan(name):
         assert q.loss()[1].item() == -inf
 
 
+@pytest.mark.parametrize("name", FORMS)
+def test_nan_in_e4m3_operands(name):
+    """A token of NaN (its rows: NaN, but 0 without a label) and a NaN in the weight (a column of every row)."""
+    with form(name):
+        p = Problem(270, 600, 64, seed=27)
+        p.labels[5], p.labels[6], p.labels[200] = 17, -1, -1
+        p.A[5, 3] = p.A[6, 63] = p.A[200, 0] = 0x7F
+        loss, lse = p.loss()
+        bad = torch.zeros(270, dtype=torch.bool, device="cuda")
+        bad[[5, 6, 200]] = True
+        assert bool(torch.isnan(lse[bad]).all()) and math.isnan(float(loss[5])) and float(loss[6]) == float(loss[200]) == 0.0
+        want, tol, want_lse, tol_lse = p.expected_loss()
+        assert bool(((lse.double() - want_lse).abs() <= tol_lse)[~bad].all()) and bool(((loss.double() - want).abs() <= tol)[~bad].all())
+        one = torch.ones(1, device="cuda")
+        for out in (F32, BF16, O52):
+            D = p.gradient(out, lse, one)
+            D = D.view(torch.float8_e5m2).float() if out == O52 else D.float()
+            assert bool(torch.isnan(D[5]).all()) and bool((D[p.labels < 0] == 0).all()) and bool(torch.isfinite(D[~bad]).all())
+        p = Problem(270, 600, 64, seed=28)
+        good = p.loss()[1].clone()
+        p.B[599, 8] = 0xFF
+        loss, lse = p.loss(z_weight=1e-2)
+        assert bool(torch.isnan(lse).all()) and bool((loss[p.labels < 0] == 0).all()) and bool(torch.isnan(loss[p.labels >= 0]).all())
+        D = p.gradient(F32, good, one)
+        assert bool((D[p.labels < 0] == 0).all()) and bool(torch.isnan(D[p.labels >= 0][:, 599]).all()) and bool(torch.isfinite(D[:, :599]).all())
+
+
+@pytest.mark.parametrize("name", FORMS)
+def test_negative_factors(name):
+    with form(name):
+        p = Problem(300, 600, 128, seed=29)
+        p.sA.neg_()
+        p.z = -p.z
+        p.check_loss(z_weight=1e-3)
+        p.check_gradient(F32, each=True)
+
+
 @pytest.mark.parametrize("name", ["chosen", "fma", "small_32x64", "tiled_256", "tiled_128"])
 @pytest.mark.parametrize("spread", [1e-3, 60.0, 3000.0])
 def test_flat_and_peaked_rows(name, spread):

@@ -42,7 +42,8 @@ def test_what_both_products_refuse(wrong, word):
 @pytest.mark.parametrize("wrong,word", [
     (dict(loss=None), "loss"), (dict(loss=Z + 2), "loss"), (dict(lse=None), "NULL"), (dict(lse=Z + 2), "aligned"), (dict(workspace=None), "workspace"),
     (dict(workspace=W + 4), "workspace"), (dict(workspace_bytes=8 * M * 2 - 1), "workspace"), (dict(lse=Z), "overlap"), (dict(lse=Z + 4 * (M - 1)), "overlap"),
-    (dict(workspace=Z), "overlap"), (dict(labels=Z), "overlap"), (dict(labels=W + 8), "overlap")])
+    (dict(workspace=Z), "overlap"), (dict(labels=Z), "overlap"), (dict(labels=W + 8), "overlap"),
+    (dict(loss=A + 4), "overlap"), (dict(lse=B + N * K - 4), "overlap"), (dict(workspace=F), "overlap")])
 def test_what_the_loss_refuses(wrong, word):
     assert xent(**wrong) == BAD and word in fp8.fp8_last_error(), fp8.fp8_last_error()
 
