@@ -5,6 +5,8 @@
 #include "gemm_loss.hpp"
 #include "gemm_op_epilogue.hpp"
 
+#include <cfloat>
+
 namespace fp8mm {
 namespace {
 
@@ -142,7 +144,9 @@ __device__ __forceinline__ void loss_store_gradient(v16f (&acc)[NB][4], uint8_t*
         const int row = wave_m0 + mb * 32 + (l & 31);
         const bool none = part.label == -1;
         // (of a row without a label 2^-infinity times 0; what is infinite or NaN itself is taken out below)
-        const float nlse2 = none ? -__builtin_inff() : -part.lse2, scale = none ? 0.0f : part.scale;
+        // FP8 outputs: y sD, with sD in the row's factors (held within the finite numbers); the maximum is divided by it at the end.
+        const float nlse2 = none ? -__builtin_inff() : -part.lse2, scale = none ? 0.0f : FP8OUT ? __builtin_amdgcn_fmed3f(part.scale * sD, -FLT_MAX, FLT_MAX) : part.scale;
+        const float dloss = FP8OUT ? part.dloss * sD : part.dloss;
         const int64_t from = part.label - wave_n0;
         const int label = from >= 0 && from < WN ? (int)from : -1;
         float x[NB * 16];
@@ -161,7 +165,7 @@ __device__ __forceinline__ void loss_store_gradient(v16f (&acc)[NB][4], uint8_t*
             for (int i = 0; i < 16; ++i) y[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[nb * 16 + i], UNIFORM ? f2 : kLog2e, nlse2)) * scale;
             if (__any(label >> 5 == nb)) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) y[i] = label == loss_column(nb * 16 + i, h) ? y[i] - part.dloss : y[i];
+                for (int i = 0; i < 16; ++i) y[i] = label == loss_column(nb * 16 + i, h) ? y[i] - dloss : y[i];
             }
             unsigned most = max_bits_of<16>(y);
             if (__any(none && most != 0)) {
@@ -188,11 +192,9 @@ __device__ __forceinline__ void loss_store_gradient(v16f (&acc)[NB][4], uint8_t*
                     *LDS_PTR(v2i, dst + 8 * q * ESZ) = p;
                 }
             } else {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) y[i] *= sD;
-                // (as in the plain epilogue: the largest product tells whether anything has to be clamped or looked at)
+                // (as in the plain epilogue: the largest value tells whether anything has to be clamped or looked at)
                 u32x4 p;
-                if (__all(__builtin_fabsf(as_f32(most) * sD) <= (FMT == FP8_E4M3 ? 448.0f : 57344.0f))) {
+                if (__all(as_f32(most) <= (FMT == FP8_E4M3 ? 448.0f : 57344.0f))) {
 #pragma unroll
                     for (int q = 0; q < 4; ++q) p[q] = encode4_inside<FMT>(y[4 * q], y[4 * q + 1], y[4 * q + 2], y[4 * q + 3]);
                 } else {
@@ -232,7 +234,8 @@ __device__ __forceinline__ void loss_store_gradient(v16f (&acc)[NB][4], uint8_t*
         // (unasked: 256 workgroups that end together queue up for a look at the cell longer than for the atomic itself, whose end nobody waits for)
         if (w == 0 && l == 0) {
             const u32x4 all = *LDS_PTR(u32x4, cells);
-            atomicMax((unsigned*)o.amax_out, max(max(all[0], all[1]), max(all[2], all[3])));
+            const unsigned most = max(max(all[0], all[1]), max(all[2], all[3]));
+            atomicMax((unsigned*)o.amax_out, FP8OUT ? as_u32(__builtin_fabsf(as_f32(most) / sD)) : most);
         }
     }
 }
