@@ -10,24 +10,35 @@
 namespace fp8mm {
 namespace {
 
-// What the tile's end needs of a lane's four rows, asked for while the last stage is multiplied (registers of the stage before are free then).
-template <int NB, int OP>
+// What the tile's end needs of its 256 rows: a thread asks for one row's while the last stage is multiplied, in four registers, and leaves it in LDS when the
+// slabs are done with.  (A lane's own four rows, in sixteen registers, spilled 92 bytes of every thread: the gradient of 4096 x 50257 x 2048 762 us instead of 737.)
+template <int OP>
 struct LossRows {
-    int64_t label[4];
-    float lse[4], dloss[4];
+    int64_t label;
+    float lse, dloss;
     __device__ __forceinline__ void fetch(const LossArgs& o, int M, int m0, int w)
     {
-        const int l = (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
-#pragma unroll
-        for (int mb = 0; mb < 4; ++mb) {
-            const int row = min(m0 + (w >> 1) * 128 + mb * 32 + (l & 31), M - 1);
-            label[mb] = o.labels[row];
-            if (OP == 5) { lse[mb] = o.lse[row]; dloss[mb] = o.dloss[o.dloss_per_row ? row : 0]; }
+        const int row = min(m0 + w * 64 + (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)), M - 1);
+        label = o.labels[row];
+        if (OP == 5) { lse = o.lse[row]; dloss = o.dloss[o.dloss_per_row ? row : 0]; }
+    }
+    // (behind a barrier; ends with one)
+    __device__ __forceinline__ void leave(const LossArgs& o, int N, uint8_t* smem, int w) const
+    {
+        const int row = w * 64 + (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+        const int64_t c = column_of_label(o, label);
+        const int column = c < N ? (int)c : -2;
+        if (OP == 4) {
+            *LDS_PTR(int, smem + OP_ROW_FACTORS + row * 4) = column;
+        } else {
+            const LossRow r = loss_row(o, lse, dloss, label);
+            *LDS_PTR(v4f, smem + OP_ROW_FACTORS + row * 16) = (v4f){r.lse2, r.scale, r.dloss, as_f32((unsigned)column)};
         }
+        __syncthreads();
     }
 };
-template <int NB> struct OpTouch<NB, 4> : LossRows<NB, 4> { };
-template <int NB> struct OpTouch<NB, 5> : LossRows<NB, 5> { };
+template <int NB> struct OpTouch<NB, 4> : LossRows<4> { };
+template <int NB> struct OpTouch<NB, 5> : LossRows<5> { };
 
 // The sums of the wave's rows 32 mb .. 32 mb + 31.  (The ends below walk the four blocks of rows in a loop: unrolled, a tile's end was four times the code, which
 // every tile fetches anew.)
@@ -47,8 +58,6 @@ __device__ __forceinline__ void sums_of(const v16f (&acc)[NB][4], int mb, float 
         default: take(std::integral_constant<int, 3>{}); break;
     }
 }
-// One of a lane's four values.
-template <class T> __device__ __forceinline__ T row_of(const T (&v)[4], int mb) { return mb == 0 ? v[0] : mb == 1 ? v[1] : mb == 2 ? v[2] : v[3]; }
 // The column of a lane's value i of its row, of lanes h = 0 .. 31 and 32 .. 63.
 __device__ __forceinline__ int loss_column(int i, int h) { return (i >> 4) * 32 + ((i >> 2) & 3) * 8 + 4 * h + (i & 3); }
 
@@ -56,7 +65,7 @@ __device__ __forceinline__ int loss_column(int i, int h) { return (i >> 4) * 32 
 // row's pair over the wave's columns takes one exchange between lanes, and no logit goes through LDS.
 // PLAIN: one positive factor for all, no columns outside.
 template <int NB, bool PLAIN>
-__device__ __forceinline__ void loss_store_pairs(v16f (&acc)[NB][4], uint8_t* smem, const LossArgs& o, const LossRows<NB, 4>& rows, double a_all, double b_all, int M, int N, int wave_m0,
+__device__ __forceinline__ void loss_store_pairs(v16f (&acc)[NB][4], uint8_t* smem, const LossArgs& o, double a_all, double b_all, int M, int N, int wave_m0,
                                                  int wave_n0, int w, int l)
 {
     const int h = l >> 5;
@@ -74,8 +83,8 @@ __device__ __forceinline__ void loss_store_pairs(v16f (&acc)[NB][4], uint8_t* sm
 #pragma unroll 1
     for (int mb = 0; mb < 4; ++mb) {
         const int row = wave_m0 + 32 * mb + (l & 31);
-        const int64_t from = column_of_label(o, row_of(rows.label, mb)) - wave_n0;
-        const int label = from >= 0 && from < min(32 * NB, N - wave_n0) ? (int)from : -1;
+        const int column = *LDS_PTR(int, smem + OP_ROW_FACTORS + ((w >> 1) * 128 + 32 * mb + (l & 31)) * 4);
+        const int label = column >= wave_n0 && column < wave_n0 + 32 * NB ? column - wave_n0 : -1;
         float t[NB * 16];
         sums_of<NB>(acc, mb, t);
         if (!PLAIN) {
@@ -100,15 +109,15 @@ __device__ __forceinline__ void loss_store_pairs(v16f (&acc)[NB][4], uint8_t* sm
 }
 
 template <int NB>
-__device__ __forceinline__ void loss_store_pairs(v16f (&acc)[NB][4], uint8_t* smem, const LossArgs& o, const LossRows<NB, 4>& rows, int M, int N, int m0, int n0, int w)
+__device__ __forceinline__ void loss_store_pairs(v16f (&acc)[NB][4], uint8_t* smem, const LossArgs& o, int M, int N, int m0, int n0, int w)
 {
     const int l = (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));      // (see store_tile)
     const int wave_m0 = m0 + (w >> 1) * 128, wave_n0 = n0 + (w & 1) * (32 * NB);
     if (wave_n0 >= N) return;
     const double a_all = o.a_per_row ? 1.0 : 1.0 / (double)op_scalar(o.sA_dev), b_all = o.b_factors == B_ONE ? 1.0 / (double)op_scalar(o.sB_dev) : 1.0;
     // (the largest logit belongs to the largest sum where the factor is positive)
-    if (wave_n0 + 32 * NB <= N && !o.a_per_row && o.b_factors == B_ONE && a_all * b_all > 0.0) loss_store_pairs<NB, true>(acc, smem, o, rows, a_all, b_all, M, N, wave_m0, wave_n0, w, l);
-    else loss_store_pairs<NB, false>(acc, smem, o, rows, a_all, b_all, M, N, wave_m0, wave_n0, w, l);
+    if (wave_n0 + 32 * NB <= N && !o.a_per_row && o.b_factors == B_ONE && a_all * b_all > 0.0) loss_store_pairs<NB, true>(acc, smem, o, a_all, b_all, M, N, wave_m0, wave_n0, w, l);
+    else loss_store_pairs<NB, false>(acc, smem, o, a_all, b_all, M, N, wave_m0, wave_n0, w, l);
 }
 
 // The gradient: as the plain epilogue leaves outputs, everything in the registers that hold the sums, where a lane's row is one of four, and converted before the
@@ -116,12 +125,12 @@ __device__ __forceinline__ void loss_store_pairs(v16f (&acc)[NB][4], uint8_t* sm
 // the feed-forward operators do: 4096 x 50257 x 2048 to E5M2 754 us.)
 // UNIFORM: one factor for all.
 template <int OUT, int NB, bool UNIFORM>
-__device__ __forceinline__ void loss_store_gradient(v16f (&acc)[NB][4], uint8_t* smem, const LossArgs& o, const LossRows<NB, 5>& rows, void* D, int M, int N, int m0, int n0, int w)
+__device__ __forceinline__ void loss_store_gradient(v16f (&acc)[NB][4], uint8_t* smem, const LossArgs& o, void* D, int M, int N, int m0, int n0, int w)
 {
     constexpr bool FP8OUT = OUT == OUT_E4M3 || OUT == OUT_E5M2;
     constexpr int FMT = OUT == OUT_E5M2 ? FP8_E5M2 : FP8_E4M3, ESZ = OUT == OUT_F32 ? 4 : OUT == OUT_BF16 ? 2 : 1;
     constexpr int WN = 32 * NB, ROWB = WN * ESZ + 16, LANES = WN * ESZ / 16, ROWS = 64 / LANES;      // of the turned block: bytes of a row, its lanes, rows a store
-    static_assert(4 * 32 * ROWB <= OP_COLUMN_FACTORS && 64 % LANES == 0 && 32 % ROWS == 0, "room for the turned rows; whole rows");
+    static_assert(4 * 32 * ROWB <= OP_ROW_FACTORS && 64 % LANES == 0 && 32 % ROWS == 0, "room for the turned rows; whole rows");
     const int l = (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));      // (see store_tile)
     const int h = l >> 5, wave_m0 = m0 + (w >> 1) * 128, wave_n0 = n0 + (w & 1) * WN;
     const bool n_edge = wave_n0 + WN > N;
@@ -140,15 +149,14 @@ __device__ __forceinline__ void loss_store_gradient(v16f (&acc)[NB][4], uint8_t*
     unsigned top = 0;
 #pragma unroll
     for (int mb = 0; mb < 4; ++mb) {
-        const LossRow part = loss_row(o, row_of(rows.lse, mb), row_of(rows.dloss, mb), row_of(rows.label, mb));
-        const int row = wave_m0 + mb * 32 + (l & 31);
-        const bool none = part.label == -1;
+        const v4f part = *LDS_PTR(v4f, smem + OP_ROW_FACTORS + ((w >> 1) * 128 + 32 * mb + (l & 31)) * 16);
+        const int row = wave_m0 + mb * 32 + (l & 31), column = (int)as_u32(part[3]);
+        const bool none = column == -1;
         // (of a row without a label 2^-infinity times 0; what is infinite or NaN itself is taken out below)
         // FP8 outputs: y sD, with sD in the row's factors (held within the finite numbers); the maximum is divided by it at the end.
-        const float nlse2 = none ? -__builtin_inff() : -part.lse2, scale = none ? 0.0f : FP8OUT ? __builtin_amdgcn_fmed3f(part.scale * sD, -FLT_MAX, FLT_MAX) : part.scale;
-        const float dloss = FP8OUT ? part.dloss * sD : part.dloss;
-        const int64_t from = part.label - wave_n0;
-        const int label = from >= 0 && from < WN ? (int)from : -1;
+        const float nlse2 = none ? -__builtin_inff() : -part[0], scale = none ? 0.0f : FP8OUT ? __builtin_amdgcn_fmed3f(part[1] * sD, -FLT_MAX, FLT_MAX) : part[1];
+        const float dloss = FP8OUT ? part[2] * sD : part[2];
+        const int label = column >= wave_n0 && column < wave_n0 + WN ? column - wave_n0 : -1;
         float x[NB * 16];
 #pragma unroll
         for (int i = 0; i < NB * 16; ++i) x[i] = acc[i >> 4][mb][i & 15];
@@ -241,22 +249,23 @@ __device__ __forceinline__ void loss_store_gradient(v16f (&acc)[NB][4], uint8_t*
 }
 
 template <int OUT, int NB>
-__device__ __forceinline__ void loss_store_gradient(v16f (&acc)[NB][4], uint8_t* smem, const LossArgs& o, const LossRows<NB, 5>& rows, void* D, int M, int N, int m0, int n0, int w)
+__device__ __forceinline__ void loss_store_gradient(v16f (&acc)[NB][4], uint8_t* smem, const LossArgs& o, void* D, int M, int N, int m0, int n0, int w)
 {
-    if (!o.a_per_row && o.b_factors == B_ONE) loss_store_gradient<OUT, NB, true>(acc, smem, o, rows, D, M, N, m0, n0, w);
-    else loss_store_gradient<OUT, NB, false>(acc, smem, o, rows, D, M, N, m0, n0, w);
+    if (!o.a_per_row && o.b_factors == B_ONE) loss_store_gradient<OUT, NB, true>(acc, smem, o, D, M, N, m0, n0, w);
+    else loss_store_gradient<OUT, NB, false>(acc, smem, o, D, M, N, m0, n0, w);
 }
 
 // OP of the tile: 4 the loss, 5 its gradient.
 template <int NB, int OP>
-__device__ __forceinline__ void loss_store_tile(v16f (&acc)[NB][4], uint8_t* smem, const LossArgs& o, const LossRows<NB, OP>& rows, void* D, int M, int N, int m0, int n0, int w)
+__device__ __forceinline__ void loss_store_tile(v16f (&acc)[NB][4], uint8_t* smem, const LossArgs& o, const LossRows<OP>& rows, void* D, int M, int N, int m0, int n0, int w)
 {
-    if constexpr (OP == 4) loss_store_pairs<NB>(acc, smem, o, rows, M, N, m0, n0, w);
+    rows.leave(o, N, smem, w);
+    if constexpr (OP == 4) loss_store_pairs<NB>(acc, smem, o, M, N, m0, n0, w);
     else switch (o.out_kind) {
-        case OUT_F32: loss_store_gradient<OUT_F32, NB>(acc, smem, o, rows, D, M, N, m0, n0, w); break;
-        case OUT_BF16: loss_store_gradient<OUT_BF16, NB>(acc, smem, o, rows, D, M, N, m0, n0, w); break;
-        case OUT_E4M3: loss_store_gradient<OUT_E4M3, NB>(acc, smem, o, rows, D, M, N, m0, n0, w); break;
-        default: loss_store_gradient<OUT_E5M2, NB>(acc, smem, o, rows, D, M, N, m0, n0, w); break;
+        case OUT_F32: loss_store_gradient<OUT_F32, NB>(acc, smem, o, D, M, N, m0, n0, w); break;
+        case OUT_BF16: loss_store_gradient<OUT_BF16, NB>(acc, smem, o, D, M, N, m0, n0, w); break;
+        case OUT_E4M3: loss_store_gradient<OUT_E4M3, NB>(acc, smem, o, D, M, N, m0, n0, w); break;
+        default: loss_store_gradient<OUT_E5M2, NB>(acc, smem, o, D, M, N, m0, n0, w); break;
     }
 }
 
