@@ -5,8 +5,6 @@
 #include "gemm_loss.hpp"
 #include "gemm_op_epilogue.hpp"
 
-#include <cfloat>
-
 namespace fp8mm {
 namespace {
 
@@ -142,7 +140,19 @@ __device__ __forceinline__ void loss_store_gradient(v16f (&acc)[NB][4], uint8_t*
         for (int i = 0; i < (NB + 1) / 2; ++i)
             if (64 * i + l < WN) *LDS_PTR(double, columns + 64 * i + l) = 1.0 / (double)o.sB_dev[min(wave_n0 + 64 * i + l, N - 1)];
     }
+    // FP8 outputs: y sD with sD in the rows' parts, and the maximum divided by it at the end (4096 x 50257 x 2048 762 -> 751 us); where a part could overflow, or a
+    // small maximum be lost, the outputs are multiplied one by one, on the way that also takes what has to be clamped.  (As an instance of its own: 744 -> 765.)
     const float sD = FP8OUT && o.sD_dev ? op_scalar(o.sD_dev) : 1.0f;
+    bool inside = true;
+    if (FP8OUT) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const v4f part = *LDS_PTR(v4f, smem + OP_ROW_FACTORS + ((w >> 1) * 128 + 64 * i + l) * 16);
+            inside &= (int)as_u32(part[3]) == -1 || (__builtin_fabsf(part[1] * sD) < __builtin_inff() && __builtin_fabsf(part[2] * sD) < __builtin_inff());
+        }
+    }
+    const bool folded = FP8OUT && __builtin_fabsf(sD) >= 1.0f && __all(inside);
+    const float fold = folded ? sD : 1.0f, limit = !folded ? -1.0f : FMT == FP8_E4M3 ? 448.0f : 57344.0f;
     uint8_t* blk = smem + w * (32 * ROWB);
     uint8_t* d_wave = (uint8_t*)D + ((size_t)wave_m0 * N + wave_n0) * ESZ;
     const int st_row = l / LANES, st_col = (l % LANES) * 16, left = N - (wave_n0 + st_col / ESZ);
@@ -153,9 +163,8 @@ __device__ __forceinline__ void loss_store_gradient(v16f (&acc)[NB][4], uint8_t*
         const int row = wave_m0 + mb * 32 + (l & 31), column = (int)as_u32(part[3]);
         const bool none = column == -1;
         // (of a row without a label 2^-infinity times 0; what is infinite or NaN itself is taken out below)
-        // FP8 outputs: y sD, with sD in the row's factors (held within the finite numbers); the maximum is divided by it at the end.
-        const float nlse2 = none ? -__builtin_inff() : -part[0], scale = none ? 0.0f : FP8OUT ? __builtin_amdgcn_fmed3f(part[1] * sD, -FLT_MAX, FLT_MAX) : part[1];
-        const float dloss = FP8OUT ? part[2] * sD : part[2];
+        const float nlse2 = none ? -__builtin_inff() : -part[0], scale = none ? 0.0f : FP8OUT ? part[1] * fold : part[1];
+        const float dloss = FP8OUT ? part[2] * fold : part[2];
         const int label = column >= wave_n0 && column < wave_n0 + WN ? column - wave_n0 : -1;
         float x[NB * 16];
 #pragma unroll
@@ -202,10 +211,14 @@ __device__ __forceinline__ void loss_store_gradient(v16f (&acc)[NB][4], uint8_t*
             } else {
                 // (as in the plain epilogue: the largest value tells whether anything has to be clamped or looked at)
                 u32x4 p;
-                if (__all(as_f32(most) <= (FMT == FP8_E4M3 ? 448.0f : 57344.0f))) {
+                if (__all(as_f32(most) <= limit)) {
 #pragma unroll
                     for (int q = 0; q < 4; ++q) p[q] = encode4_inside<FMT>(y[4 * q], y[4 * q + 1], y[4 * q + 2], y[4 * q + 3]);
                 } else {
+                    if (!folded) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) y[i] *= sD;
+                    }
                     p = encode16<FMT, kCastCvt>(y);
                 }
 #pragma unroll
@@ -237,13 +250,12 @@ __device__ __forceinline__ void loss_store_gradient(v16f (&acc)[NB][4], uint8_t*
 #pragma unroll
         for (int d = 32; d >= 1; d >>= 1) top = max(top, (unsigned)__shfl_xor((int)top, d, 64));
         unsigned* cells = (unsigned*)(smem + OP_AMAX);
-        if (l == 0) *LDS_PTR(unsigned, cells + w) = top;
+        if (l == 0) *LDS_PTR(unsigned, cells + w) = folded ? as_u32(__builtin_fabsf(as_f32(top) / sD)) : top;
         __syncthreads();
         // (unasked: 256 workgroups that end together queue up for a look at the cell longer than for the atomic itself, whose end nobody waits for)
         if (w == 0 && l == 0) {
             const u32x4 all = *LDS_PTR(u32x4, cells);
-            const unsigned most = max(max(all[0], all[1]), max(all[2], all[3]));
-            atomicMax((unsigned*)o.amax_out, FP8OUT ? as_u32(__builtin_fabsf(as_f32(most) / sD)) : most);
+            atomicMax((unsigned*)o.amax_out, max(max(all[0], all[1]), max(all[2], all[3])));
         }
     }
 }

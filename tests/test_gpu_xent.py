@@ -327,6 +327,35 @@ def test_nan_in_e4m3_operands(name):
 
 
 @pytest.mark.parametrize("name", FORMS)
+@pytest.mark.parametrize("sD,dloss", [(0.0, 1.0), (math.inf, 1.0), (math.nan, 1.0), (2.0 ** -140, 1.0), (2.0 ** -60, 1.0), (2.0 ** 126, 8.0), (-(2.0 ** 126), 8.0), (2.0 ** 100, 2.0 ** 29)])
+def test_factors_of_the_output_far_from_one(name, sD, dloss):
+    """All of a piece's probabilities are 2^-96 of a softmax, as of rows whose label is in another piece: dloss sD of 2^129, beyond fp32, where outputs are inside E5M2;
+    outputs that vanish beside a maximum that does not; factors of 0, infinity and NaN.  y is off by what check_gradient counts, its product with sD rounds once more."""
+    M, N, K = 260, 300, 32
+    with form(name):
+        p = Problem(M, N, K, seed=29, first=1000)
+        p.labels.fill_(3)
+        p.labels[7] = -1
+        lse = (torch.logsumexp(p.z, 1) + 96.0 * math.log(2.0)).float()
+        d, cell, s = torch.full((1,), dloss, device="cuda"), torch.full((1,), 7.0, device="cuda"), torch.full((1,), sD, device="cuda")
+        for amax in (cell, None):
+            D = p.gradient(O52, lse, d, 0.0, s, amax).view(torch.float8_e5m2).double()
+            y, tol = p.expected_gradient(lse, d)
+            # what underflows: an exponential below the smallest normal number, 2^-126, is 0 (a logit 20.8 below its row's sum is): dloss 2^-126 in place of 1e-36
+            tol = tol + torch.where(p.labels < 0, 0, dloss * 2.0 ** -126 - 1e-36)[:, None]
+            if math.isfinite(sD):
+                y8, tol8 = (y * sD).clamp(-57344, 57344), tol * abs(sD)
+                half = torch.maximum((y8.abs() + tol8) * 2.0 ** -3, torch.full_like(y8, 2.0 ** -17))
+                assert bool(((D - y8).abs() <= tol8 + half + 2.0 ** -23 * y8.abs()).all())
+            elif math.isnan(sD):
+                assert bool(torch.isnan(D[p.labels >= 0]).all())
+            else:
+                full = y >= 2.0 ** -125                                              # (y infinity is one, which E5M2 holds; 0 infinity is none)
+                assert bool((D[full] == math.inf).all()) and int(full.sum()) > 0.99 * 259 * N and not bool(torch.isfinite(D[p.labels >= 0]).any())
+        assert abs(float(cell) - float(y.max())) <= float(tol.max()) + 2.0 ** -23 * float(y.max())
+
+
+@pytest.mark.parametrize("name", FORMS)
 def test_negative_factors(name):
     with form(name):
         p = Problem(300, 600, 128, seed=29)
