@@ -317,6 +317,8 @@ int launch_gemm_loss(const GemmArgs& g, const LossArgs& args, float* loss, float
     typedef int (*any_fn)(const GemmArgs&, const LossArgs&, int);
     static const any_fn any[4] = {launch_loss_any_l0, launch_loss_any_l1, launch_loss_any_l2, launch_loss_any_l3};
     static const tiled_fn tiled[2][2] = {{launch_loss_tiled_l0_a0, launch_loss_tiled_l0_a1}, {launch_loss_tiled_l1_a0, launch_loss_tiled_l1_a1}};
+    // (a workgroup of 256 threads joins 32 rows; asked before the product is launched)
+    if (args.op == OP_LOSS && g.M > (int64_t)(UINT32_MAX / 256) * 32) return fail(FP8_ERR_UNSUPPORTED, "fp8_gemm_xent: %lld rows exceed the grid limit", (long long)g.M);
     LossArgs o = args;
     int64_t blocks = 0;                                      // of columns, with a pair each for every row
     OpPlan plan{};

@@ -62,6 +62,12 @@ def test_sizes_beyond_what_bytes_can_be_counted():
         assert call(M=1 << 35, N=1 << 35) == UNSUPPORTED
 
 
+def test_more_rows_than_can_be_joined():
+    """Refused before the product is launched, where a launch would fail for want of a device."""
+    rows = 32 * ((1 << 32) // 256 - 1) + 1
+    assert xent(M=rows, N=1, K=0, A=None, B=None, lse=Z + (1 << 36), workspace_bytes=1 << 40) == UNSUPPORTED and "grid limit" in fp8.fp8_last_error()
+
+
 def test_workspace_size():
     size = fp8.fp8_gemm_xent_workspace_size
     assert [size(5, n) for n in (0, 1, 32, 33, 50257)] == [40, 80, 80, 120, 5 * 8 * (1571 + 1)]
