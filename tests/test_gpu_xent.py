@@ -327,7 +327,14 @@ def test_nan_in_e4m3_operands(name):
 
 
 @pytest.mark.parametrize("name", FORMS)
-@pytest.mark.parametrize("sD,dloss", [(0.0, 1.0), (math.inf, 1.0), (math.nan, 1.0), (2.0 ** -140, 1.0), (2.0 ** -60, 1.0), (2.0 ** 126, 8.0), (-(2.0 ** 126), 8.0), (2.0 ** 100, 2.0 ** 29)])
+def test_factors_of_the_output_below_one(name):
+    with form(name):
+        for each in (False, True):
+            Problem(270, 700, 64, seed=30, rows=each).check_gradient(O43, each=each, sD=torch.full((1,), 0.25, device="cuda"))
+
+
+@pytest.mark.parametrize("name", FORMS)
+@pytest.mark.parametrize("sD,dloss", [(0.0, 1.0), (math.inf, 1.0), (math.nan, 1.0), (2.0 ** -140, 1.0), (2.0 ** -60, 1.0), (2.0 ** 126, 8.0), (-(2.0 ** 126), 8.0), (2.0 ** 100, 2.0 ** 29), (2.0 ** -20, 2.0 ** 30)])
 def test_factors_of_the_output_far_from_one(name, sD, dloss):
     """All of a piece's probabilities are 2^-96 of a softmax, as of rows whose label is in another piece: dloss sD of 2^129, beyond fp32, where outputs are inside E5M2;
     outputs that vanish beside a maximum that does not; factors of 0, infinity and NaN.  y is off by what check_gradient counts, its product with sD rounds once more."""
