@@ -532,7 +532,8 @@ int fp8_gemm_xent_grad(const uint8_t* A, int fmtA, int transA, const uint8_t* B,
 
 /*
  * fp8_adamw -- one step of AdamW on `count` tensors, with the gradients' clipping, states in 32 bits or in FP8, and the new weights in FP8:
- *     g  = grad * min(1, max_norm / (norm + 1e-6))           (norm given; as fp8_grad_clip, nothing is written to grad)
+ *     g  = grad * min(1, max_norm * (1 / (norm + 1e-6)))     (norm given; nothing is written to grad.  Reciprocal and product are rounded one after the other, as torch does with a
+ *                                                             number over a tensor: the factor may be an ulp or two, some for norms beyond 2^126, off fp8_grad_clip's, the quotient)
  *     m' = beta1 m + (1 - beta1) g;   v' = beta2 v + (1 - beta2) g^2
  *     p' = p - lr (weight_decay p + (m' / (1 - beta1^t)) / (sqrt(v' / (1 - beta2^t)) + eps)),  t = *step
  *     q  = encode(fl32(p' * q_scale)),  q_amax = max |p'|     (p' before it is rounded to p's type)

@@ -1,6 +1,6 @@
 // AdamW over many tensors at once, with the gradients' clipping, states in 32 bits or in FP8, and FP8 copies of the new weights, for gfx950 (MI355X).
 //
-//   g = c grad, c = min(1, max_norm / (norm + 1e-6)) or 1
+//   g = c grad, c = min(1, max_norm (1 / (norm + 1e-6))) or 1
 //   m' = b1 m + (1 - b1) g,   v' = b2 v + (1 - b2) g^2
 //   p' = p - lr (wd p + (m' / (1 - b1^t)) / (sqrt(v' / (1 - b2^t)) + eps))
 //   q = encode(p' s),  amax = max |p'|
@@ -351,7 +351,9 @@ __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(AdamTensors list, A
     if (a.norm) {
         const float n = *a.norm;
         if (a.skip_nonfinite && !(__builtin_fabsf(n) < __builtin_inff())) return;
-        s.clip = a.max_norm / (n + 1e-6f);
+        // (Not the quotient: a number over a tensor in torch is this, and a factor that differs by an ulp makes a fifth of all m' do, and now and then an element round the
+        // other way: where it is a block's largest, the block's next factor differs by a fourteenth.)
+        s.clip = a.max_norm * (1.0f / (n + 1e-6f));
         if (s.clip > 1.0f) s.clip = 1.0f;        // (NaN stays)
         if (n == __builtin_inff()) s.clip = 0.0f;
     }
