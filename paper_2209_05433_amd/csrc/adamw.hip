@@ -168,14 +168,34 @@ __device__ __forceinline__ float block_factor(const float (&x)[4], bool& finite)
     return finite && f < __builtin_inff() ? f : 1.0f;          // (f of 0 is infinite)
 }
 
-// The square root to the nearest for normal numbers (an ulp off below them): the instruction's is an ulp off, so its neighbours are looked at.
-__device__ __forceinline__ float root(float x)
+// The square root of a normal number, 0, infinity or NaN to the nearest: the instruction's is an ulp off, so its neighbours are looked at.
+__device__ __forceinline__ float root_of_normal(float x)
 {
     float s = __builtin_amdgcn_sqrtf(x);
     const float below = as_f32(as_u32(s) - 1u), above = as_f32(as_u32(s) + 1u);
     const float at_below = __builtin_fmaf(-below, s, x), at_above = __builtin_fmaf(-above, s, x);
     s = at_below <= 0.0f ? below : s;
     return at_above > 0.0f ? above : s;        // (0, infinity and NaN: every comparison is false)
+}
+
+// The square roots of four numbers.  The instruction takes what lies below 2^-126 for 0: in a wave with such a number (a block that no gradient has reached for
+// long: sqrt(v) of 1e-19 would be left as the smallest code with factor 1, 2e-3) all are brought up by 2^64, and their roots down by 2^32, which is exact.
+__device__ __forceinline__ void roots(const float (&x)[4], float (&r)[4])
+{
+    unsigned least = as_u32(x[0]) - 1u;        // (0 wraps round)
+#pragma unroll
+    for (int i = 1; i < 4; ++i) least = min(least, as_u32(x[i]) - 1u);
+    if (__any(least < 0x007fffffu)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const bool below = x[i] < 0x1p-126f;
+            const float s = root_of_normal(below ? x[i] * 0x1p64f : x[i]);
+            r[i] = below ? s * 0x1p-32f : s;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = root_of_normal(x[i]);
+    }
 }
 
 // Four finite values as E4M3, rounded stochastically by 16 bits each in the upper halves of r (the lower ones 0).
@@ -276,8 +296,11 @@ __device__ __forceinline__ unsigned adam_chunk(const AdamChunk& c, const AdamSca
         }
         moments(s, g[u], m[u], v[u]);
         float r[4];
+        if (STATES8) roots(v[u], r);
+        else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) r[i] = STATES8 ? root(v[u][i]) : __builtin_amdgcn_sqrtf(v[u][i]);
+            for (int i = 0; i < 4; ++i) r[i] = __builtin_amdgcn_sqrtf(v[u][i]);
+        }
         weights(s, c.decay, m[u], r, p[u]);
         if (STATES8) {
             // (what lies beyond the tensor's end is 0 in m and r)
