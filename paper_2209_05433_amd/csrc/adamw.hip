@@ -60,7 +60,11 @@ struct AdamScalars {
 static_assert(sizeof(AdamTensors) + sizeof(AdamScalars) < 4000, "kernel arguments");
 
 // What is the same for all elements.
-struct AdamStep { float clip, b1, o1, b2, o2, lr, k, eps; };      // (the update is m' / (k r + eps), with 1 / (1 - b1^t) in k and eps)
+// (the update is m' / (k r + eps), with 1 / (1 - b1^t) in k and eps)
+struct AdamStep {
+    float clip, b1, o1, b2, o2, lr, k, eps;
+    bool small_eps;         // a root of less than 2^-63 counts beside eps
+};
 
 __device__ __forceinline__ double power(double b, uint64_t t)
 {
@@ -296,8 +300,8 @@ __device__ __forceinline__ unsigned adam_chunk(const AdamChunk& c, const AdamSca
         }
         moments(s, g[u], m[u], v[u]);
         float r[4];
-        if (STATES8) roots(v[u], r);
-        else {
+        if (STATES8 || s.small_eps) roots(v[u], r);
+        else {              // (one below 2^-63 as 0: half an ulp of eps at most)
 #pragma unroll
             for (int i = 0; i < 4; ++i) r[i] = __builtin_amdgcn_sqrtf(v[u][i]);
         }
@@ -387,6 +391,7 @@ __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(AdamTensors list, A
     s.lr = *a.lr;
     s.k = (float)(c1 / __builtin_sqrt(c2));
     s.eps = (float)(c1 * (double)a.eps);
+    s.small_eps = !(s.eps >= s.k * 0x1p-38f);
     __shared__ unsigned tops[kAdamThreads / 64];
     // neighbouring chunks, so that a workgroup's maximum is of one tensor mostly
     const unsigned share = chunks / gridDim.x, rest = chunks % gridDim.x, b = blockIdx.x;

@@ -1,4 +1,4 @@
-"""AdamW to the last bit, and where its numbers leave the ordinary range: second moments below the smallest normal number.
+"""AdamW to the last bit, and where its numbers leave the ordinary range: second moments below the smallest normal number, with eps = 0 too.
 
 Tolerances as in test_gpu_adamw.py, u = 2^-24; below 2^-126 every rounding is off by up to 2^-150 instead: v' has at most five (the square of sqrt(v) as stored, two products of the
 gradient's square, b2 v, the sum), and is off by 16u v' + 5 2^-150."""
@@ -91,3 +91,26 @@ def test_a_block_without_gradients_decays(beta2):
     fp8.fp8_adamw([p], [g], [m], [v], cells(steps + 1, torch.int64), cells(1e-2), 0.9, beta2, 0.0, m_scale=[ms], v_scale=[vs], seed=6)
     want = -1e-2 * 0.1 / math.sqrt(1 - beta2)
     assert bool(((p.double() - want).abs() <= 64 * U * abs(want) + abs(want) * 0.9 ** steps).all())
+
+
+@pytest.mark.parametrize("p_dtype", [torch.float32, torch.bfloat16])
+def test_states_in_32_bits_without_eps(p_dtype):
+    """v' from 2^-120 down to 2^-148, eps = 0: the weights move by what the formula says.  v' is off by 16u v' + 5 2^-150, the update by what that makes of it and 32u."""
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    n = 5000
+    v = torch.exp2(-120 - 28 * torch.rand(n, generator=gen, device="cuda").double()).float()
+    m = torch.randn(n, generator=gen, device="cuda") * v.double().sqrt().float()
+    g = torch.zeros(n, device="cuda")
+    g[::2] = (v[::2].double().sqrt() * 3).float()
+    p = torch.ones(n, device="cuda").to(p_dtype)
+    m0, v0, g0 = m.double(), v.double(), g.double()
+    fp8.fp8_adamw([p], [g], [m], [v], cells(7, torch.int64), cells(1e-2), 0.9, 0.95, 0.0)
+    m1, v1 = 0.9 * m0 + (1 - 0.9) * g0, 0.95 * v0 + (1 - 0.95) * g0 * g0
+    m_tol, v_tol = 16 * U * ((0.9 * m0).abs() + ((1 - 0.9) * g0).abs()) + STEP0, 16 * U * v1 + STEP0
+    assert bool(((m.double() - m1).abs() <= m_tol).all()) and bool(((v.double() - v1).abs() <= v_tol).all())
+    k1, k2 = 1 / (1 - 0.9 ** 7), (1 - 0.95 ** 7) ** 0.5
+    u = 1e-2 * k1 * k2 * m1 / v1.sqrt()
+    far = 1e-2 * k1 * k2 * ((m1.abs() + m_tol) / (v1 - v_tol).clamp(min=2.0 ** -150).sqrt() - m1.abs() / v1.sqrt())
+    want = 1.0 - u
+    tol = far + 32 * U * u.abs() + U * want.abs() + (2.0 ** -8 * want.abs() if p_dtype == torch.bfloat16 else 0)
+    assert bool(torch.isfinite(p).all()) and bool(((p.double() - want).abs() <= tol * 1.01).all()), ((p.double() - want).abs() / tol).max()
