@@ -289,7 +289,9 @@ __device__ __forceinline__ unsigned adam_chunk(const AdamChunk& c, const AdamSca
         const unsigned e = (u * kAdamThreads + threadIdx.x) * 4;
         const int left = left_of(e);
         if (STATES8) {
-            const float im = inverse(fm[u]), ir = inverse(fr[u]);
+            float im = inverse(fm[u]), ir = inverse(fr[u]);
+            // (a factor below 2^-126 or beyond 2^126, of a block that has nearly vanished: the division itself)
+            if (__any(max(as_u32(fm[u]) - 0x00800000u, as_u32(fr[u]) - 0x00800000u) > 0x7e800000u - 0x00800000u)) { im = 1.0f / fm[u]; ir = 1.0f / fr[u]; }
             typedef float f2 __attribute__((ext_vector_type(2)));
             const f2 m01 = __builtin_amdgcn_cvt_pk_f32_fp8((int)mw[u], false), m23 = __builtin_amdgcn_cvt_pk_f32_fp8((int)mw[u], true);
             const f2 r01 = __builtin_amdgcn_cvt_pk_f32_fp8((int)rw[u], false), r23 = __builtin_amdgcn_cvt_pk_f32_fp8((int)rw[u], true);

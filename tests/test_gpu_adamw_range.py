@@ -1,4 +1,5 @@
-"""AdamW to the last bit, and where its numbers leave the ordinary range: second moments below the smallest normal number, with eps = 0 too.
+"""AdamW to the last bit, and where its numbers leave the ordinary range: second moments below the smallest normal number, with eps = 0 too, factors whose
+reciprocal lies there.
 
 Tolerances as in test_gpu_adamw.py, u = 2^-24; below 2^-126 every rounding is off by up to 2^-150 instead: v' has at most five (the square of sqrt(v) as stored, two products of the
 gradient's square, b2 v, the sum), and is off by 16u v' + 5 2^-150."""
@@ -114,3 +115,39 @@ def test_states_in_32_bits_without_eps(p_dtype):
     want = 1.0 - u
     tol = far + 32 * U * u.abs() + U * want.abs() + (2.0 ** -8 * want.abs() if p_dtype == torch.bfloat16 else 0)
     assert bool(torch.isfinite(p).all()) and bool(((p.double() - want).abs() <= tol * 1.01).all()), ((p.double() - want).abs() / tol).max()
+
+
+@pytest.mark.parametrize("which", ["m", "v"])
+def test_factors_whose_reciprocal_is_not_normal(which):
+    """m = byte / factor for every finite factor > 0, 2^127 and 3e38 among them, and the smallest; elements of 0 beside."""
+    factors = torch.tensor([2.0 ** 126, 1.5 * 2.0 ** 126, 2.0 ** 127, 3e38, 2.0 ** -126, 2.0 ** -127, 2.0 ** -120], device="cuda")
+    n = len(factors) * BLOCK
+    codes = torch.zeros(n, device="cuda")
+    codes.view(-1, BLOCK)[:, ::3] = 1.0
+    codes.view(-1, BLOCK)[:, 1] = 448.0 if which == "m" else 2.0
+    codes = codes.to(F8)
+    p, g = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
+    zero, one = torch.zeros(n, dtype=torch.uint8, device="cuda"), torch.ones(len(factors), device="cuda")
+    state, scale = codes.view(torch.uint8).clone(), factors.clone()
+    m, ms, v, vs = (state, scale, zero, one) if which == "m" else (zero, one, state, scale)
+    x0 = codes.double() / factors.double().repeat_interleave(BLOCK)
+    # eps of 1: with v = 0 the weights move by lr m' / (1 - beta1^t) = 2 m'; a reciprocal below 2^-126 is off by up to 2^-22 of itself, 4u
+    fp8.fp8_adamw([p], [g], [m], [v], cells(1, torch.int64), cells(1.0), 0.5, 0.25, 1.0, m_scale=[ms], v_scale=[vs], seed=7)
+    if which == "m":
+        x1 = 0.5 * x0
+        fine = x0 < 3e38              # (beyond: 448 2^120 = 6e38, which is m and the step of p, is no number in 32 bits)
+        assert bool(((p.double() + 2 * x1)[fine].abs() <= 32 * U * x1[fine] + 4 * STEP0).all()), (p.double().view(-1, BLOCK)[:, 1], x1.view(-1, BLOCK)[:, 1])
+    else:
+        # (v' of factors this large is 0; of the smallest ones it is infinite, and r with it)
+        x1 = 0.5 * x0
+        x1 = torch.where(x0 * x0 < 2.0 ** -150, torch.zeros_like(x1), x1)
+        fine = x0 * x0 < 3e38
+        assert not bool(p.any())
+    got = state.view(F8).double() / scale.double().repeat_interleave(BLOCK)
+    top = x1.view(-1, BLOCK).amax(1, keepdim=True).expand(-1, BLOCK).reshape(-1)
+    # (a block whose factor would not be finite: factor 1, where these are rounded to 0)
+    kept = 448.0 / top.clamp(min=1e-300) < 3.4e38
+    want = torch.where(kept, x1, torch.zeros_like(x1))
+    inside = fine.view(-1, BLOCK).all(1).repeat_interleave(BLOCK)
+    assert bool(((got - want).abs()[inside] <= 2.0 ** -3 * want[inside] + 2.0 ** -9 / 448 * top[inside] * kept[inside]).all())
+    assert bool((scale.double().repeat_interleave(BLOCK)[inside & ~kept] == 1).all()) and bool((scale[4:] > 0).all())
