@@ -60,9 +60,10 @@ struct AdamScalars {
 static_assert(sizeof(AdamTensors) + sizeof(AdamScalars) < 4000, "kernel arguments");
 
 // What is the same for all elements.
-// (the update is m' / (k r + eps), with 1 / (1 - b1^t) in k and eps)
+// (the update is m' / (k r + eps), with 1 / (1 - b1^t) in k and eps.  Both are times `unit`, 1 but where the denominator may have no normal reciprocal: k is at least 2^-54
+// and k r less than 2^92, so by an eps below 2^-126, where the unit is 2^30, or near 2^126, where it is 2^-30)
 struct AdamStep {
-    float clip, b1, o1, b2, o2, lr, k, eps;
+    float clip, b1, o1, b2, o2, lr, k, eps, unit;
     bool small_eps;         // a root of less than 2^-63 counts beside eps
 };
 
@@ -239,7 +240,7 @@ __device__ __forceinline__ void weights(const AdamStep& s, float decay, const fl
 {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float u = m[i] * __builtin_amdgcn_rcpf(__builtin_fmaf(r[i], s.k, s.eps));
+        const float u = m[i] * __builtin_amdgcn_rcpf(__builtin_fmaf(r[i], s.k, s.eps)) * s.unit;
         p[i] = __builtin_fmaf(-s.lr, __builtin_fmaf(decay, p[i], u), p[i]);
     }
 }
@@ -391,9 +392,11 @@ __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(AdamTensors list, A
     s.b2 = (float)a.beta2; s.o2 = (float)(1.0 - a.beta2);
     const double c1 = 1.0 - power(a.beta1, (uint64_t)t_step), c2 = 1.0 - power(a.beta2, (uint64_t)t_step);
     s.lr = *a.lr;
-    s.k = (float)(c1 / __builtin_sqrt(c2));
-    s.eps = (float)(c1 * (double)a.eps);
-    s.small_eps = !(s.eps >= s.k * 0x1p-38f);
+    const double k = c1 / __builtin_sqrt(c2), eps = c1 * (double)a.eps, unit = eps < 0x1p-126 ? 0x1p30 : eps > 0x1p125 ? 0x1p-30 : 1.0;
+    s.k = (float)(k * unit);
+    s.eps = (float)(eps * unit);
+    s.unit = (float)unit;
+    s.small_eps = !(eps >= k * 0x1p-38);
     __shared__ unsigned tops[kAdamThreads / 64];
     // neighbouring chunks, so that a workgroup's maximum is of one tensor mostly
     const unsigned share = chunks / gridDim.x, rest = chunks % gridDim.x, b = blockIdx.x;

@@ -1,5 +1,5 @@
 """AdamW to the last bit, and where its numbers leave the ordinary range: second moments below the smallest normal number, with eps = 0 too, factors whose
-reciprocal lies there.
+reciprocal lies there, denominators that have no normal reciprocal.
 
 Tolerances as in test_gpu_adamw.py, u = 2^-24; below 2^-126 every rounding is off by up to 2^-150 instead: v' has at most five (the square of sqrt(v) as stored, two products of the
 gradient's square, b2 v, the sum), and is off by 16u v' + 5 2^-150."""
@@ -151,3 +151,26 @@ def test_factors_whose_reciprocal_is_not_normal(which):
     inside = fine.view(-1, BLOCK).all(1).repeat_interleave(BLOCK)
     assert bool(((got - want).abs()[inside] <= 2.0 ** -3 * want[inside] + 2.0 ** -9 / 448 * top[inside] * kept[inside]).all())
     assert bool((scale.double().repeat_interleave(BLOCK)[inside & ~kept] == 1).all()) and bool((scale[4:] > 0).all())
+
+
+@pytest.mark.parametrize("states8", [False, True])
+@pytest.mark.parametrize("eps,m0", [(1e-40, 2.0 ** -136), (2e-38, 2.0 ** -120), (2.5e38, 1e38), (2.0 ** 127, 2.0 ** 125), (1e-30, 1e-30)])
+def test_denominators_without_a_normal_reciprocal(states8, eps, m0):
+    """v = 0: the update is lr (m' / (1 - beta1^t)) / eps.  1 - beta1^t is 3/4; eps times it is off by 2^-24 of itself or 2^-150."""
+    n = 300
+    p, g = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
+    if states8:
+        m, v = torch.zeros(n, dtype=torch.uint8, device="cuda"), torch.zeros(n, dtype=torch.uint8, device="cuda")
+        factor = min(256.0 / m0, 2.0 ** 127)
+        code = torch.tensor([m0 * factor], dtype=torch.float64).float().to(F8)
+        m0 = float(code.double()) / float(torch.tensor(factor).float())
+        m.fill_(int(code.view(torch.uint8)))
+        more = dict(m_scale=[torch.full((3,), factor, device="cuda")], v_scale=[torch.ones(3, device="cuda")])
+    else:
+        m, v, more = torch.full((n,), m0, device="cuda"), torch.zeros(n, device="cuda"), {}
+        m0 = float(m[0])
+    fp8.fp8_adamw([p], [g], [m], [v], cells(2, torch.int64), cells(1e-2), 0.5, 0.5, eps, **more)
+    e = float(torch.tensor(eps))
+    want = -1e-2 * (0.5 * m0 / 0.75) / e
+    tol = abs(want) * (32 * U + 2.0 ** -149 / (0.75 * e))
+    assert bool(((p.double() - want).abs() <= tol).all()), (p[0].item(), want)
