@@ -523,7 +523,7 @@ int fp8_gemm_xent(const uint8_t* A, int fmtA, int transA, const uint8_t* B, int 
  * B the piece's rows of the weight, N their number, first the first one; fp8_gemm_act with the residual in place adds up the tokens' gradient.
  *   lse     device, M fp32 values: of the whole vocabulary, as fp8_gemm_xent leaves them
  *   dloss   device, ndloss fp32 values: the gradient of each row's loss (ndloss = M) or of all (1)
- *   D, out_kind, sD_dev, amax_out  as for fp8_gemm_fused.  D must not overlap any other argument.
+ *   D, out_kind, sD_dev, amax_out  as for fp8_gemm_fused.  Neither D nor amax_out may overlap any other argument.
  * The rest as for fp8_gemm_xent.  Beyond what z_ij is off by, the exponential is within 2^-22 (|z_ij| + |lse_i| + 4) of itself.
  */
 int fp8_gemm_xent_grad(const uint8_t* A, int fmtA, int transA, const uint8_t* B, int fmtB, int transB, void* D, int out_kind, int64_t M, int64_t N, int64_t K,

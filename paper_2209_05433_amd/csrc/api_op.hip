@@ -79,7 +79,7 @@ int64_t bytes_of(int64_t rows, int64_t cols, int size)
 }
 
 // Whether np bytes from p on and nq from q on share memory.
-bool overlap(const void* p, int64_t np, const void* q, int64_t nq) { return p && q && (uintptr_t)p < (uintptr_t)q + nq && (uintptr_t)q < (uintptr_t)p + np; }
+bool overlap(const void* p, int64_t np, const void* q, int64_t nq) { return p && q && np > 0 && nq > 0 && (uintptr_t)p < (uintptr_t)q + nq && (uintptr_t)q < (uintptr_t)p + np; }
 
 int check_tensors(const char* who, int count, const void* const* x, const size_t* n, const int* dtype)
 {
@@ -246,9 +246,12 @@ int fp8_gemm_xent_grad(const uint8_t* A, int fmtA, int transA, const uint8_t* B,
     if (ndloss != 1 && ndloss != M) return fail(FP8_ERR_INVALID_ARG, "%s: ndloss = %lld is neither 1 nor M", who, (long long)ndloss);
     if (M > 0 && (!lse || !dloss || ((uintptr_t)lse | (uintptr_t)dloss) % 4)) return fail(FP8_ERR_INVALID_ARG, "%s: lse or dloss is NULL or misaligned", who);
     const int64_t d_bytes = bytes_of(M, N, out_elem_size(out_kind));
-    if (overlap(D, d_bytes, labels, 8 * M) || overlap(D, d_bytes, lse, 4 * M) || overlap(D, d_bytes, dloss, 4 * ndloss) || overlap(D, d_bytes, A, bytes_of(M, K, 1)) ||
-        overlap(D, d_bytes, B, bytes_of(K, N, 1)))
-        return fail(FP8_ERR_INVALID_ARG, "%s: D overlaps another argument", who);
+    const struct { const void* p; int64_t bytes; } in[] = {{A, bytes_of(M, K, 1)}, {B, bytes_of(K, N, 1)}, {labels, 8 * M}, {lse, 4 * M}, {dloss, 4 * ndloss}, {sA_dev, 4 * nsA},
+                                                           {sB_dev, 4 * nsB}, {sD_dev, 4}, {amax_out, 4}};
+    for (const auto& x : in)
+        if (overlap(D, d_bytes, x.p, x.bytes)) return fail(FP8_ERR_INVALID_ARG, "%s: D overlaps another argument", who);
+    for (int i = 0; i < 4; ++i)
+        if (overlap(amax_out, 4, in[i].p, in[i].bytes)) return fail(FP8_ERR_INVALID_ARG, "%s: amax_out overlaps an operand, labels or lse", who);
     o.lse = lse; o.dloss = dloss; o.dloss_per_row = ndloss == M && M != 1;
     return launch_gemm_loss(g, o, nullptr, nullptr);
 }
