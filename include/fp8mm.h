@@ -538,7 +538,8 @@ int fp8_gemm_xent_grad(const uint8_t* A, int fmtA, int transA, const uint8_t* B,
  *     p' = p - lr (weight_decay p + (m' / (1 - beta1^t)) / (sqrt(v' / (1 - beta2^t)) + eps)),  t = *step
  *     q  = encode(fl32(p' * q_scale)),  q_amax = max |p'|     (p' before it is rounded to p's type)
  * p, g, m, v, m_scale, v_scale, q, n, p_dtype, g_dtype and weight_decay are HOST arrays of `count` entries (read before the call returns).  p, m, v are updated in
- * place.  Tensors are contiguous and may start anywhere their element may; no two may overlap, and none may be in the list twice.
+ * place.  Tensors are contiguous and may start anywhere their element may.  What is written (p, m, v, m_scale, v_scale, q, q_amax) may overlap nothing else that the call
+ * reads or writes, and no weight may be in the list twice; gradients may share memory.
  *   p, p_dtype  the weights, n[i] elements, fp8_dtype_t; g, g_dtype: their gradients
  *   state_kind  FP8_STATE_F32: m[i], v[i] are n[i] fp32 values.
  *               FP8_STATE_FP8: n[i] bytes of E4M3 each, of m and of sqrt(v), and m_scale[i], v_scale[i] ceil(n[i] / 128) fp32 factors, one for each 128 elements:

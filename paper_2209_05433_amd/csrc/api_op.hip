@@ -2,8 +2,8 @@
 #include "gemm_loss.hpp"
 
 #include <algorithm>
+#include <cstdio>
 #include <exception>
-#include <utility>
 #include <vector>
 
 using namespace fp8mm;
@@ -91,6 +91,74 @@ int check_tensors(const char* who, int count, const void* const* x, const size_t
         if (n[i] > 0 && !x[i]) return fail(FP8_ERR_INVALID_ARG, "%s: x[%d] is NULL with n = %zu", who, i, n[i]);
         if (n[i] > 0 && (uintptr_t)x[i] % (dtype[i] == FP8_F32 ? 4 : 2)) return fail(FP8_ERR_INVALID_ARG, "%s: x[%d] is not aligned to its element size", who, i);
     }
+    return FP8_OK;
+}
+
+// What a step writes must be nothing else that it reads or writes, of the same tensor or another (tied weights that are in the list twice would be updated by
+// two workgroups at once).  Sorted by address, neither a range that is written may begin before the end of any other one, nor any range before the end of one that is written.
+struct MemoryRange { uintptr_t begin, end; int kind, index; };
+const char* const kAdamMemory[] = {"p", "g", "m", "v", "q", "m_scale", "v_scale", "lr", "step", "norm", "q_scale", "q_amax"};
+int check_adamw_memory(const char* who, int count, void* const* p, const int* p_dtype, const void* const* g, const int* g_dtype, const size_t* n, void* const* m, void* const* v,
+                       bool states8, float* const* m_scale, float* const* v_scale, uint8_t* const* q, const float* lr, const int64_t* step, const float* norm, const float* q_scale,
+                       const float* q_amax)
+{
+    std::vector<MemoryRange> all, merged;
+    try {
+        const size_t most = (size_t)std::max(count, 0) * (states8 ? 7 : 5) + 5;
+        all.reserve(most);
+        merged.reserve(most);
+        // one list of tensors behind the other: each is in the order of its addresses already as a rule, and joined to those before by a merge
+        auto add = [&](int kind, auto begin_of, auto bytes_of_each) {
+            const size_t first = all.size();
+            for (int i = 0; i < count; ++i) {
+                const uintptr_t at = n[i] ? (uintptr_t)begin_of(i) : 0;
+                if (at) all.push_back({at, at + bytes_of_each(i), kind, i});
+            }
+            auto less = [](const MemoryRange& a, const MemoryRange& b) { return a.begin < b.begin; };
+            if (!std::is_sorted(all.begin() + first, all.end(), less)) std::sort(all.begin() + first, all.end(), less);
+            if (first == 0 || first == all.size() || !less(all[first], all[first - 1])) return;
+            merged.resize(all.size());
+            std::merge(all.begin(), all.begin() + first, all.begin() + first, all.end(), merged.begin(), less);
+            all.swap(merged);
+        };
+        auto blocks = [&](int i) { return 4 * ((n[i] + FP8_STATE_BLOCK - 1) / FP8_STATE_BLOCK); };
+        const size_t state = states8 ? 1 : 4;
+        add(0, [&](int i) { return p[i]; }, [&](int i) { return n[i] * (p_dtype[i] == FP8_F32 ? 4 : 2); });
+        add(1, [&](int i) { return g[i]; }, [&](int i) { return n[i] * (g_dtype[i] == FP8_F32 ? 4 : 2); });
+        add(2, [&](int i) { return m[i]; }, [&](int i) { return n[i] * state; });
+        add(3, [&](int i) { return v[i]; }, [&](int i) { return n[i] * state; });
+        if (q) add(4, [&](int i) { return q[i]; }, [&](int i) { return n[i]; });
+        if (states8) add(5, [&](int i) { return m_scale[i]; }, blocks);
+        if (states8) add(6, [&](int i) { return v_scale[i]; }, blocks);
+        if (all.empty()) return FP8_OK;
+        const struct { const void* p; size_t bytes; } single[] = {{lr, 4}, {step, 8}, {norm, 4}, {q ? q_scale : nullptr, 4 * (size_t)count}, {q_amax, 4 * (size_t)count}};
+        for (int k = 0; k < 5; ++k) {
+            if (!single[k].p) continue;
+            const MemoryRange x = {(uintptr_t)single[k].p, (uintptr_t)single[k].p + single[k].bytes, 7 + k, -1};
+            all.insert(std::upper_bound(all.begin(), all.end(), x, [](const MemoryRange& a, const MemoryRange& b) { return a.begin < b.begin; }), x);
+        }
+    } catch (const std::exception&) {
+        return fail(FP8_ERR_UNSUPPORTED, "%s: no host memory for a list of %d tensors", who, count);
+    }
+    auto written = [](const MemoryRange& x) { return x.kind != 1 && x.kind < 7; };
+    auto named = [](const MemoryRange& x, char (&to)[32]) {
+        if (x.index < 0) std::snprintf(to, sizeof to, "%s", kAdamMemory[x.kind]);
+        else std::snprintf(to, sizeof to, "%s[%d]", kAdamMemory[x.kind], x.index);
+        return to;
+    };
+    char one[32], two[32];
+    const MemoryRange* furthest = nullptr;                 // of those before
+    const MemoryRange* furthest_written = nullptr;
+    for (const MemoryRange& x : all) {
+        const MemoryRange* other = written(x) ? furthest : furthest_written;
+        if (other && x.begin < other->end)
+            return fail(FP8_ERR_INVALID_ARG, "%s: %s%s and %s overlap", who, x.kind == 0 && other->kind == 0 ? "two of the weights, " : "", named(*other, one), named(x, two));
+        if (!furthest || x.end > furthest->end) furthest = &x;
+        if (written(x) && (!furthest_written || x.end > furthest_written->end)) furthest_written = &x;
+    }
+    // (the maxima: no tensor that is written holds them, as seen above, nor a gradient)
+    for (int i = 0; q_amax && i < count; ++i)
+        if (n[i] && overlap(q_amax, 4 * (int64_t)count, g[i], (int64_t)n[i] * (g_dtype[i] == FP8_F32 ? 4 : 2))) return fail(FP8_ERR_INVALID_ARG, "%s: g[%d] and q_amax overlap", who, i);
     return FP8_OK;
 }
 
@@ -286,25 +354,8 @@ int fp8_adamw(int count, void* const* p, const int* p_dtype, const void* const* 
         if (!m[i] || !v[i] || (uintptr_t)m[i] % state || (uintptr_t)v[i] % state) return fail(FP8_ERR_INVALID_ARG, "%s: m[%d] or v[%d] is NULL or misaligned", who, i, i);
         if (states8 && (!m_scale[i] || !v_scale[i] || ((uintptr_t)m_scale[i] | (uintptr_t)v_scale[i]) % 4))
             return fail(FP8_ERR_INVALID_ARG, "%s: m_scale[%d] or v_scale[%d] is NULL or misaligned", who, i, i);
-        // (what one tensor's update reads and writes)
-        const int64_t k = (int64_t)n[i], blocks = 4 * ((k + FP8_STATE_BLOCK - 1) / FP8_STATE_BLOCK);
-        const struct { const void* p; int64_t bytes; } of[] = {{p[i], k * (p_dtype[i] == FP8_F32 ? 4 : 2)}, {g[i], k * (g_dtype[i] == FP8_F32 ? 4 : 2)}, {m[i], k * state}, {v[i], k * state},
-                                                               {q ? q[i] : nullptr, k}, {states8 ? m_scale[i] : nullptr, blocks}, {states8 ? v_scale[i] : nullptr, blocks}};
-        for (size_t a = 0; a < sizeof of / sizeof *of; ++a)
-            for (size_t b = 0; b < a; ++b)
-                if (overlap(of[a].p, of[a].bytes, of[b].p, of[b].bytes)) return fail(FP8_ERR_INVALID_ARG, "%s: arguments of tensor %d overlap", who, i);
     }
-    // A weight that is in the list twice (tied weights) would be updated by two workgroups at once.
-    std::vector<std::pair<uintptr_t, uintptr_t>> taken;
-    try {
-        for (int i = 0; i < count; ++i)
-            if (n[i]) taken.emplace_back((uintptr_t)p[i], (uintptr_t)p[i] + n[i] * (p_dtype[i] == FP8_F32 ? 4 : 2));
-        std::sort(taken.begin(), taken.end());
-    } catch (const std::exception&) {
-        return fail(FP8_ERR_UNSUPPORTED, "%s: no host memory for a list of %d tensors", who, count);
-    }
-    for (size_t i = 1; i < taken.size(); ++i)
-        if (taken[i].first < taken[i - 1].second) return fail(FP8_ERR_INVALID_ARG, "%s: two of the weights share memory", who);
+    if (int e = check_adamw_memory(who, count, p, p_dtype, g, g_dtype, n, m, v, states8, m_scale, v_scale, q, lr, step, norm, q_scale, q_amax)) return e;
     AdamwArgs a{};
     a.count = count; a.p = p; a.p_dtype = p_dtype; a.g = g; a.g_dtype = g_dtype; a.n = n; a.m = m; a.v = v;
     a.states8 = states8; a.m_scale = m_scale; a.v_scale = v_scale; a.seed = seed;
