@@ -190,7 +190,7 @@ __device__ __forceinline__ void roots(const float (&x)[4], float (&r)[4])
     unsigned least = as_u32(x[0]) - 1u;        // (0 wraps round)
 #pragma unroll
     for (int i = 1; i < 4; ++i) least = min(least, as_u32(x[i]) - 1u);
-    if (__any(least < 0x007fffffu)) {
+    if (__builtin_expect(__any(least < 0x007fffffu), 0)) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const bool below = x[i] < 0x1p-126f;
@@ -292,7 +292,7 @@ __device__ __forceinline__ unsigned adam_chunk(const AdamChunk& c, const AdamSca
         if (STATES8) {
             float im = inverse(fm[u]), ir = inverse(fr[u]);
             // (a factor below 2^-126 or beyond 2^126, of a block that has nearly vanished: the division itself)
-            if (__any(max(as_u32(fm[u]) - 0x00800000u, as_u32(fr[u]) - 0x00800000u) > 0x7e800000u - 0x00800000u)) { im = 1.0f / fm[u]; ir = 1.0f / fr[u]; }
+            if (__builtin_expect(__any(max(as_u32(fm[u]) - 0x00800000u, as_u32(fr[u]) - 0x00800000u) > 0x7e800000u - 0x00800000u), 0)) { im = 1.0f / fm[u]; ir = 1.0f / fr[u]; }
             typedef float f2 __attribute__((ext_vector_type(2)));
             const f2 m01 = __builtin_amdgcn_cvt_pk_f32_fp8((int)mw[u], false), m23 = __builtin_amdgcn_cvt_pk_f32_fp8((int)mw[u], true);
             const f2 r01 = __builtin_amdgcn_cvt_pk_f32_fp8((int)rw[u], false), r23 = __builtin_amdgcn_cvt_pk_f32_fp8((int)rw[u], true);
@@ -327,7 +327,7 @@ __device__ __forceinline__ unsigned adam_chunk(const AdamChunk& c, const AdamSca
                     y[i] = r[i] > 0.0f ? __builtin_fmaxf(y[i], 0.001953125f) : y[i];
                 }
                 unsigned wm, wr;
-                if (finite) { wm = encode_states(x, low); wr = encode_states(y, bits); }
+                if (__builtin_expect(finite, 1)) { wm = encode_states(x, low); wr = encode_states(y, bits); }
                 else { wm = encode_any_states(x, low); wr = encode_any_states(y, bits); }
                 store4_bytes((uint8_t*)c.m + e, left, wm);
                 store4_bytes((uint8_t*)c.v + e, left, wr);
