@@ -39,7 +39,7 @@ class Head:
         self.m, self.v = ([new(vocabulary * width, dtype=torch.uint8 if self.states8 else torch.float32) for _ in range(2)] for _ in range(2))
         blocks = (vocabulary * width + fp8.FP8_STATE_BLOCK - 1) // fp8.FP8_STATE_BLOCK
         self.scales = [[torch.ones(blocks, device="cuda") for _ in range(2)] for _ in range(2)]
-        self.qW, self.qW_scale, self.qW_amax = new(vocabulary, width, dtype=torch.uint8), torch.ones(2, device="cuda"), new(2)
+        self.qW, self.qW_scale, self.qW_amax, self.next_scale = new(vocabulary, width, dtype=torch.uint8), torch.ones(2, device="cuda"), new(2), new(2)
         self.step, self.lr = new(1, dtype=torch.int64), new(1)
         # the tokens' vectors
         self.qx, self.x_amax, self.x_scale = new(tokens, width, dtype=torch.uint8), new(1), torch.ones(1, device="cuda")
@@ -77,10 +77,13 @@ class Head:
 
     def update(self, lr, max_norm=1.0):
         """One step of AdamW; the norm before clipping."""
-        self.step.add_(1)
         self.lr.fill_(lr)
-        fp8.fp8_scale_from_amax_n(self.qW_amax, E4M3, self.qW_scale)
         fp8.fp8_grad_norm(self.grads, self.norm, self.norm_workspace)
+        # a norm that is not finite leaves weights, states and FP8 bytes as they are: the count too, and the factor that the bytes were made by (decided on the device, for graphs)
+        goes = torch.isfinite(self.norm)
+        self.step.add_(goes)
+        fp8.fp8_scale_from_amax_n(self.qW_amax, E4M3, self.next_scale)
+        self.qW_scale.copy_(torch.where(goes, self.next_scale, self.qW_scale))
         states = dict(m_scale=self.scales[0], v_scale=self.scales[1], seed=17) if self.states8 else {}
         fp8.fp8_adamw(self.params, self.grads, self.m, self.v, self.step, self.lr, 0.9, 0.95, 1e-8, [0.0, 0.01], self.norm, max_norm, q=[None, self.qW], q_scale=self.qW_scale,
                       q_amax=self.qW_amax, flags=fp8.FP8_ADAMW_SKIP_NONFINITE, **states)

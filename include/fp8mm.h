@@ -555,7 +555,8 @@ int fp8_gemm_xent_grad(const uint8_t* A, int fmtA, int transA, const uint8_t* B,
  *   q           NULL, or n[i] bytes or NULL for each tensor: FP8 copies in q_fmt (fp8_format_t), saturating
  *   q_scale     device, `count` fp32 factors (of tensors without a copy not looked at); needed with q
  *   q_amax      device, `count` fp32 values, or NULL.  Written, not accumulated; 0 of tensors without a copy
- *   flags       FP8_ADAMW_SKIP_NONFINITE: an infinite or NaN norm leaves everything as it is (else as for fp8_grad_clip)
+ *   flags       FP8_ADAMW_SKIP_NONFINITE: an infinite or NaN norm leaves everything as it is (else as for fp8_grad_clip).  A caller that counts the step or computes
+ *               q_scale before the call takes both back then, or does so only for a finite norm: q still belongs to the factors that it was written with
  * Computed in 32 bits, m', v' rounding every sum and product once.  Results are the same in every run.
  */
 typedef enum { FP8_STATE_F32 = 0, FP8_STATE_FP8 = 1 } fp8_state_t;
