@@ -524,7 +524,8 @@ int fp8_gemm_xent(const uint8_t* A, int fmtA, int transA, const uint8_t* B, int 
  *   lse     device, M fp32 values: of the whole vocabulary, as fp8_gemm_xent leaves them
  *   dloss   device, ndloss fp32 values: the gradient of each row's loss (ndloss = M) or of all (1)
  *   D, out_kind, sD_dev, amax_out  as for fp8_gemm_fused.  Neither D nor amax_out may overlap any other argument.
- * The rest as for fp8_gemm_xent.  Beyond what z_ij is off by, the exponential is within 2^-22 (|z_ij| + |lse_i| + 4) of itself.
+ * The rest as for fp8_gemm_xent.  Beyond what z_ij is off by, the exponential is within 2^-22 (|z_ij| + |lse_i| + 4) of itself, relative, plus 2^-126: one below the smallest normal
+ * number comes out as 0, and y_ij is off by |dloss_i (1 + 2 z_weight lse_i)| 2^-126 there.
  */
 int fp8_gemm_xent_grad(const uint8_t* A, int fmtA, int transA, const uint8_t* B, int fmtB, int transB, void* D, int out_kind, int64_t M, int64_t N, int64_t K,
                        const float* sA_dev, int64_t nsA, const float* sB_dev, int64_t nsB, const int64_t* labels, int64_t first, float z_weight,
