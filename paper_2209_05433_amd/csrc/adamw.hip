@@ -29,7 +29,7 @@ constexpr int kAdamThreads = 256, U = 4;
 constexpr unsigned kAdamChunk = kAdamThreads * 4 * U;           // elements
 constexpr unsigned kMostGrid = 1u << 16, kAllAtOnce = 4096;     // workgroups
 constexpr unsigned kParamF32 = 0x80000000u, kGradF32 = 0x40000000u;
-constexpr size_t kAdamStreamBytes = (size_t)448 << 20;
+constexpr size_t kAdamStreamBytes = (size_t)512 << 20;
 constexpr int kAdamTensors = 50;
 
 // Tensor t owns the chunks end[t - 1] .. end[t] - 1; size[t]: elements of its last chunk and the types; index[t]: its place in the caller's list.
@@ -491,8 +491,9 @@ int launch_adamw(const AdamwArgs& a)
         enqueue(adamw_clear_kernel, dim3(1), dim3(256), 0, a.stream, a.q_amax, a.count, a.norm, a.skip_nonfinite);
         if (int e = check_launch("AdamW (maxima)")) return e;
     }
-    // Loads and stores that leave the caches alone where no cache holds the tensors anyway (us, ordinary / streaming: states in 32 bits 170 MB 85.5 / 88.1, 383 MB 106 / 116,
-    // 680 MB 171 / 164, 27.2 GB 5120 / 4990; in FP8 381 MB 102 / 117, 857 MB 217 / 182, 15.2 GB 2995 / 2880).
+    // Loads and stores that leave the caches alone where no cache holds the tensors anyway (us, ordinary / streaming, with copies and maxima: states in 32 bits 266 MB 45 / 49,
+    // 383 MB 62 / 70, 482 MB 93 / 101, 574 MB 117 / 117, 673 MB 137 / 131, 1.36 GB 267 / 247, 27.2 GB 5110 / 4945; in FP8 149 MB 43 / 43, 270 MB 67 / 75, 377 MB 80 / 89,
+    // 583 MB 142 / 132, 762 MB 179 / 162, 15.2 GB 3010 / 2916).
     size_t bytes = 0;
     for (int i = 0; i < a.count; ++i)
         bytes += a.n[i] * (size_t)((a.p_dtype[i] == FP8_F32 ? 8 : 4) + (a.g_dtype[i] == FP8_F32 ? 4 : 2) + (a.states8 ? 4 : 16) + (a.q && a.q[i] ? 1 : 0));
