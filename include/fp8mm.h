@@ -547,7 +547,7 @@ int fp8_gemm_xent_grad(const uint8_t* A, int fmtA, int transA, const uint8_t* B,
  *               m = decode(byte) / factor.  A state of zeros is bytes 0 and factors 1.  The step leaves factors of 448 times the reciprocal of the block's largest magnitude
  *               (1 where that is 0 or not finite) and bytes rounded stochastically as by fp8_quantize_sr: to the neighbour above where T + r >= 2^16; r of m the low, of sqrt(v)
  *               the high half of word e % 4 of Philox4x32-10 with the counter (e / 4: two words, t's low word, i) and the key `seed`, e: the element, i: the tensor.
- *               A positive sqrt(v) never becomes 0.  Factors that are not finite and > 0 are not a state.
+ *               A positive sqrt(v') is never rounded to 0.  Factors that are not finite and > 0 are not a state.
  *   seed        of FP8 states; one for a whole run of training will do
  *   weight_decay  finite numbers >= 0, or NULL: none
  *   lr, step    device: one fp32, one int64 >= 1 (the caller counts)

@@ -8,11 +8,11 @@
 // States in FP8: m and r = sqrt(v) in E4M3, 128 elements of a tensor with one factor each for m and r.  r and not
 // v is kept, since E4M3's range of 2^18 is then one of 2^36 of v.  Both are rounded stochastically: b2 near 1 moves r by far less than half
 // a step of 3 mantissa bits at a time, so that rounding to nearest would leave it where it is for ever, while the expected value of what is stored here
-// is what was computed.  Only r > 0 never becomes 0, which would make the next step's m / (sqrt(v) + eps) one over eps.  The weights are updated from the states
+// is what was computed.  Only r > 0 is never rounded to 0, which would make the next step's m / (sqrt(v) + eps) one over eps.  The weights are updated from the states
 // before they are rounded.
 //
 // HBM bound: one pass, with everything the step needs of an element loaded once (p, g, m, v) and stored once (p, m, v, q); 27 bytes an element with states in 32 bits
-// and 15 in FP8, bf16 gradients and copies: 10^9 elements in 4.98 ms (5.46 TB/s; a copy 5.15) and 2.87 ms (5.30 TB/s, the vector ALU busy nearly all the time: the
+// and 15 in FP8, bf16 gradients and copies: 10^9 elements in 4.90 ms (5.55 TB/s; a copy 5.15) and 2.91 to 2.96 ms (5.15 to 5.23 TB/s, the vector ALU busy nearly all the time: the
 // generator's ten rounds for four elements, two factors and two roundings).
 #include "gemm_common.hpp"
 #include "cast_common.hpp"
@@ -422,7 +422,7 @@ __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(AdamTensors list, A
         top = max(top, of_chunk);
         if (a.q_amax && k.q && (c + 1 == end || c + 1 == list.end[t])) {
             // One atomic a workgroup and tensor.  Where many workgroups are behind one another most find a larger value in the cell and leave it at that; where all are
-            // at work at once they would only queue up for the look as well (864 workgroups, 96 MB: 33.8 us with it, 23.9 without, 17.8 without maxima).
+            // at work at once they would only queue up for the look as well (864 workgroups, 96 MB: 33.8 us with it, 23.6 without, 18.2 without maxima).
             __syncthreads();
 #pragma unroll
             for (int d = 32; d >= 1; d >>= 1) top = max(top, (unsigned)__shfl_xor((int)top, d, 64));

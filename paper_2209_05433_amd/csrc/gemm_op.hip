@@ -208,7 +208,8 @@ OpPlan plan_op(const GemmArgs& g, const OpArgs& o)
     }
     if (!tiled) return ((g.M + 63) / 64) * ((p.N + 63) / 64) > 0x7fffffffll ? plain_fmas : OpPlan{false, false, SMALL_64x64, acc, 0, 0, false};
     // The width whose rounds of 256 workgroups take less time, or both widths in one launch, by the plain product's model of run times with the
-    // operator's own time on top (us of a 256-wide tile: fitted to 8192 x 8192 outputs over K = 256; it is the same per output in both widths).
+    // operator's own time on top (us of a 256-wide tile: fitted to 8192 x 8192 outputs over K = 256; it is the same per output in both widths.  The loss's 1 and its
+    // gradient's 10 are what the 13 rounds of 4096 x 50257 x 2048 take longer; how the choice fares at other shapes stands below).
     const TileTimes t = tile_times(acc, 2.0 * (double)((g.K + 2 * TILE_K - 1) / (2 * TILE_K)));
     const double own = o.op == OP_LOSS ? 1.0 : loss ? 10.0 : o.op == OP_GATED_GRAD ? 25.0 : o.op == OP_GATED ? 3.0 : o.op == OP_ACT_GRAD || o.side ? 12.0 : 7.0;
     const double wide = t.wide + own, narrow = t.narrow + 0.5 * own;
@@ -223,7 +224,9 @@ OpPlan plan_op(const GemmArgs& g, const OpArgs& o)
         return r;
     }
     // (as many wide columns as whole rounds hold: fewer or more leave units idle between the widths; beyond 16 rounds the last one matters little)
-    // (the loss by 1.5 % of the model's time: 4096 x 50257 x 2048 639 -> 625 us, its gradient 767 -> 749)
+    // (the loss by 1.5 % of the model's time.  Of 11 shapes of 777 to 8192 rows, 6283 to 128000 columns and K from 512 to 8192, the loss and its gradient to E5M2, the choice is the
+    // best of it, wide, narrow and a forced share of both, or within 1.3 %; where it is both widths in one launch, at 4096 x 50257 x 2048, 2048 x 50257 x 2048, 8192 x 12564 x 2048, 5000 x
+    // 20000 x 512 and 2600 x 50257 x 8192, it takes 1.6 to 5 % less than the better single width)
     double best = (loss ? 0.985 : 0.97) * std::min(us_wide, us_narrow);
     for (int64_t units = 256; units / tiles_m < wide_all && tiles_m * wide_all <= 16 * 256; units += 256) {
         const int64_t c = std::max<int64_t>(units / tiles_m, 1);
