@@ -184,7 +184,7 @@ __device__ __forceinline__ float root_of_normal(float x)
 }
 
 // The square roots of four numbers.  The instruction takes what lies below 2^-126 for 0: in a wave with such a number (a block that no gradient has reached for
-// long: sqrt(v) of 1e-19 would be left as the smallest code with factor 1, 2e-3) all are brought up by 2^64, and their roots down by 2^32, which is exact.
+// long: sqrt(v) of 1e-19 would be left as the smallest code with factor 1, 2e-3) it is brought up by 2^64, and its root down by 2^32, which is exact.
 __device__ __forceinline__ void roots(const float (&x)[4], float (&r)[4])
 {
     unsigned least = as_u32(x[0]) - 1u;        // (0 wraps round)
