@@ -9,7 +9,7 @@
 // No logit is ever stored: a row of a tile leaves 8 bytes where its logits are 128 to 512.
 //
 // Bound by the matrix cores (one exponential beside 2 K operations, a part of the tile's end): 8192 x 50257 x 12288 at 1.51 to 1.55 PFLOP/s, 87 % of the matrix cycles busy;
-// 4096 x 50257 x 2048, where an end comes after every 32 stages, 627 to 650 us by the card (67 %) and its gradient to E5M2 742 to 764 (54 %), the product to bf16 680.
+// 4096 x 50257 x 2048, where an end comes after every 32 stages, 625 to 650 us by the card (67 %) and its gradient to E5M2 737 to 764 (54 %), the product to bf16 680.
 #pragma once
 
 #include "gemm_op.hpp"
